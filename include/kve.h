@@ -226,14 +226,16 @@ int kvE_compact_topk(kvE_store* st, int layer, int k, void* stream);
  * be covered by the keep list (kvE_compact; its tau decides "discarded").
  *   mode KVE_RECLAIM_DISCARDED: pages of chunks with s_t < tau (never attended to again);
  *   mode KVE_RECLAIM_GATED:     pages of all chunks in the range; needs cfg.attend == KVE_ATTEND_SUMMARY,
- *                               where a retained chunk is read through its one summary row.
+ *                               where a retained chunk is read through its one summary row;
+ *   mode KVE_RECLAIM_PACKED:    the bf16 pages of all chunks in the range, which need not be covered by the keep list but
+ *                               must all be held in 4 bits (kvE_pack_chunks); kvE_decode_attn_q4 does not read them.
  * free_list: DEVICE int32 [capacity], receives the page ids, sequences in order, chunks ascending;
  * free_count: DEVICE int32, receives how many.  The page_table entries handed back become -1 (the
  * library writes the caller's page table here); entries that are already -1 are skipped.  If the
  * list would not fit, nothing is handed back, *free_count is 0 and the status word gets
  * KVE_ERR_CAPACITY.  Afterwards the raw rows of those chunks are gone: summarising them again or
  * kvE_decode_attn_dense flags KVE_ERR_CAPACITY in the status word instead of reading them. */
-enum { KVE_RECLAIM_DISCARDED = 0, KVE_RECLAIM_GATED = 1 };
+enum { KVE_RECLAIM_DISCARDED = 0, KVE_RECLAIM_GATED = 1, KVE_RECLAIM_PACKED = 2 };
 int kvE_reclaim_pages(kvE_store* st, int layer, int chunk_begin, int chunk_end, int mode, int32_t* free_list,
                       int64_t capacity, int32_t* free_count, void* stream);
 
@@ -274,6 +276,92 @@ int kvE_decode_attn_dense(kvE_store* st, int layer, const void* q, void* out, fl
  *   cfg.max_query_tokens. */
 int kvE_decode_attn_block(kvE_store* st, int layer, const void* q, int n_query_tokens, int dense, int causal,
                           void* out, float* lse, float scale, void* stream);
+
+/* ---- rotary positions with the append --------------------------------------------------------------------------------
+ * The store holds keys that carry their position already.  These calls turn it into them on the way in: pair j of a row
+ * (64 pairs a row) turns by phi_j = pos[axis[j]] * inv_freq[j],  (a, b) -> (a cos phi_j - b sin phi_j, b cos phi_j + a sin phi_j),
+ * computed in fp32 (the angle reduced in 64 bits, so far positions keep their angle) and rounded to bf16 once.  Text has one
+ * axis; images and video have time, height and width, each followed by some of the pairs. */
+enum { KVE_ROPE_HALVES = 0, KVE_ROPE_ADJACENT = 1 };      /* pair j: elements (j, j + 64), or (2 j, 2 j + 1) */
+#define KVE_ROPE_MAX_AXES 4
+typedef struct {
+  int32_t n_axes;        /* 1 .. KVE_ROPE_MAX_AXES */
+  int32_t layout;        /* KVE_ROPE_* */
+  uint8_t axis[64];      /* the axis that pair j follows, < n_axes */
+  double inv_freq[64];   /* radians per position; 0: the pair is not turned */
+} kvE_rope;
+
+/* bf16 rows of d numbers as a projection leaves them: row (b, token, head) at data + b stride_b + token stride_t + head stride_h
+ * (strides in elements, multiples of 8; data on 16 bytes).  q, k and v may be parts of one tensor. */
+typedef struct {
+  const void* data;
+  int64_t stride_b, stride_t, stride_h;
+} kvE_rows;
+
+/* kvE_append of n_new tokens with rotary positions: k_new is turned and stored, v_new stored as it is, q (Hq heads; nullable, then
+ * q_out is NULL too) turned into q_out: DEVICE bf16 [B][n_new][Hq][d], the layout of kvE_decode_attn_block and kvE_decode_attn_q4
+ * (n_new == 1, Hq == Hkv: of kvE_decode_attn).  q_out may be q itself if q has that layout; otherwise they do not overlap.
+ * positions: DEVICE int32 [B][n_new][n_axes], any values, or NULL: every axis has the token's index in the cache.
+ * rope and the kvE_rows are read during the call.  One launch; errors and *n_ready as in kvE_append. */
+int kvE_append_rope(kvE_store* st, int layer, const kvE_rows* q, const kvE_rows* k_new, const kvE_rows* v_new,
+                    const int32_t* positions, int n_new, const kvE_rope* rope, void* q_out, int* n_ready, void* stream);
+
+/* The same at the length the DEVICE holds, which the call advances by n_new (as kvE_append_next: captured in a CUDA graph,
+ * every replay handles the next n_new tokens; positions are read at replay time; n_reserve as there).  A sequence without room is
+ * left alone and KVE_ERR_CAPACITY is set in the status word; q_out is written all the same. */
+int kvE_append_rope_next(kvE_store* st, int layer, const kvE_rows* q, const kvE_rows* k_new, const kvE_rows* v_new,
+                         const int32_t* positions, int n_new, int n_reserve, const kvE_rope* rope, void* q_out, void* stream);
+
+/* ---- the cache in 4 bits ---------------------------------------------------------------------------------------------
+ * Chunks that have left the window may be held in 4 bits: 144 bytes a token (key and value) instead of 512.  A row has two
+ * groups of 64 numbers; a group keeps its smallest number low, a scale s = bf16((largest - low) / 15) and per number x the code
+ * c = count of the borders low + (k + 1/2) s, k = 0..14, that lie below x (on a border: the lower code); it stands for
+ * low + c s.  Rows must be finite; a group that holds an infinity or a NaN stands for NaN throughout.
+ * Chunks [0, n_packed) of a layer have such a copy (kvE_packed_chunks); n_packed is held on the device too.  kvE_set_len to a length that cuts
+ * into them lowers it to the chunks that are still complete; a caller who writes pages himself sets the length to 0 first. */
+#define KVE_Q4_UNIT_ROWS 16       /* C must be a multiple of it */
+#define KVE_Q4_UNIT_BYTES 1152    /* of 16 rows: codes and scales */
+typedef struct {
+  void* k4_pages;         /* [n_pages4][C / 16][KVE_Q4_UNIT_BYTES], on 16 bytes; one page = one chunk of one (layer, b, h) */
+  void* v4_pages;
+  int64_t n_pages4;
+  const int32_t* page_table4;   /* [n_layers][S][max_chunks] page ids in these pools, filled by the caller */
+  int32_t max_query_tokens;     /* most query tokens per kvE_decode_attn_q4 call, times Hq / Hkv at most 128 */
+  void* workspace;        /* kvE_q4_workspace_bytes bytes, 256-byte aligned, cleared by kvE_attach_q4 */
+  size_t workspace_bytes;
+} kvE_q4_buffers;
+
+/* Bytes of kvE_q4_buffers.workspace; 0 if the geometry is not supported. */
+size_t kvE_q4_workspace_bytes(const kvE_config* cfg, int max_query_tokens);
+
+/* Gives a handle its 4-bit pages (caller-owned DEVICE buffers, borrowed until kvE_destroy); no chunk is packed afterwards, also
+ * where the handle had others before.  Synchronises the device.  KVE_ERR_GEOMETRY if C is not a multiple of 16. */
+int kvE_attach_q4(kvE_store* st, const kvE_q4_buffers* buf);
+
+/* Chunks [chunk_begin, chunk_end) of every sequence of `layer` to 4 bits, from their bf16 pages, which stay as they are
+ * (kvE_reclaim_pages with KVE_RECLAIM_PACKED hands them back).  chunk_begin <= n_packed, chunk_end <= floor((n - W) / C): else
+ * KVE_ERR_STATE.  Neither summaries nor scores are needed. */
+int kvE_pack_chunks(kvE_store* st, int layer, int chunk_begin, int chunk_end, void* stream);
+
+/* What chunks [chunk_begin, chunk_end) stand for, rounded to bf16: k_out, v_out DEVICE bf16 [S][(chunk_end - chunk_begin) C][d], on 16
+ * bytes: what kvE_append takes.  The way back, to roll into a packed chunk or to move the history elsewhere. */
+int kvE_unpack_chunks(kvE_store* st, int layer, int chunk_begin, int chunk_end, void* k_out, void* v_out, void* stream);
+
+/* Host-side view: chunks of `layer` held in 4 bits. */
+int kvE_packed_chunks(const kvE_store* st, int layer, int* n_packed);
+
+/* Eq. 1 for n_query_tokens tokens on all Hq query heads (as kvE_decode_attn_block; n_query_tokens == 1 for plain decoding, grouped
+ * heads included) over the retained set at full resolution: dense == 0: the rows of the kept chunks and every row behind the
+ * keep list; dense != 0: all n stored rows.  Rows of packed chunks are read in 4 bits, others in bf16 (kept chunks that are not packed
+ * included).  The position of the list, of the packed chunks and of the newest row are taken from the device: a captured launch
+ * stays valid across triggers and further packing.  cfg.attend does not matter.
+ *   causal != 0: the block's tokens are the newest of the cache and see it up to themselves; KVE_ERR_STATE if fewer rows than
+ *   n_query_tokens lie behind the packed and listed chunks (a replay that comes to that sets KVE_ERR_CAPACITY).
+ *   Products and sums in fp32, weights to 16 bits, one bf16 rounding of the result.  A row that sees nothing gives 0 and lse = -inf.
+ *   q, out: DEVICE bf16 [B][n_query_tokens][Hq][d], on 16 bytes; lse: DEVICE fp32 [B][n_query_tokens][Hq] or NULL.
+ *   KVE_ERR_STATE without kvE_attach_q4, KVE_ERR_CAPACITY if n_query_tokens exceeds max_query_tokens. */
+int kvE_decode_attn_q4(kvE_store* st, int layer, const void* q, int n_query_tokens, int dense, int causal, void* out, float* lse,
+                       float scale, void* stream);
 
 /* kvE_decode_attn without any scratch from the caller.  (The paper has no counterpart: this is a
  * deployment aid.)  Some users of this library must not allocate device memory once they are
@@ -333,7 +421,7 @@ int kvE_layer_state(const kvE_store* st, int layer, int* n_tokens, int* n_summar
  * kvE_refresh takes all chunks in one range, so that a duration is that of the kernel alone.  KVE_K_GATE_RNN is the
  * whole gate, the input projection included (KVE_K_GATE_PROJ: no kernel of its own, always -1). */
 enum { KVE_K_APPEND = 0, KVE_K_CHUNK_MEAN, KVE_K_CHUNK_MLP, KVE_K_GATE_PROJ, KVE_K_GATE_RNN, KVE_K_COMPACT,
-       KVE_K_ATTN, KVE_K_ATTN_DENSE, KVE_K_ATTN_BLOCK, KVE_K_COUNT };
+       KVE_K_ATTN, KVE_K_ATTN_DENSE, KVE_K_ATTN_BLOCK, KVE_K_PACK, KVE_K_ATTN_Q4, KVE_K_COUNT };
 int kvE_profile(kvE_store* st, int enable);
 int kvE_profile_read(kvE_store* st, float* us /* [KVE_K_COUNT] */);
 

@@ -26,8 +26,9 @@ STATUS = {0: "KVE_OK", -1: "KVE_ERR_ARG", -2: "KVE_ERR_GEOMETRY", -3: "KVE_ERR_C
 EXPORTS = ["kvE_workspace_bytes", "kvE_create", "kvE_destroy", "kvE_set_attend", "kvE_set_gate_planes", "kvE_append", "kvE_append_next", "kvE_set_len",
            "kvE_summarize_chunks", "kvE_gate", "kvE_gate_next", "kvE_refresh", "kvE_refresh_next", "kvE_adopt_device_state", "kvE_compact", "kvE_compact_topk", "kvE_decode_attn", "kvE_decode_step", "kvE_decode_attn_dense", "kvE_decode_attn_block",
            "kvE_decode_attn_static", "kvE_reclaim_pages", "kvE_decode_step_host", "kvE_decode_step_host_async", "kvE_poll_status", "kvE_layer_state", "kvE_last_cuda_error",
-           "kvE_profile", "kvE_profile_read", "kvE_selftest_timeout"]
-KERNEL_IDS = ["append", "chunk_mean", "chunk_mlp", "gate_proj", "gate_rnn", "compact", "attn", "attn_dense", "attn_block"]
+           "kvE_profile", "kvE_profile_read", "kvE_selftest_timeout", "kvE_append_rope", "kvE_append_rope_next", "kvE_q4_workspace_bytes", "kvE_attach_q4",
+           "kvE_pack_chunks", "kvE_unpack_chunks", "kvE_packed_chunks", "kvE_decode_attn_q4"]
+KERNEL_IDS = ["append", "chunk_mean", "chunk_mlp", "gate_proj", "gate_rnn", "compact", "attn", "attn_dense", "attn_block", "pack", "attn_q4"]
 
 
 class KveError(RuntimeError):
@@ -58,6 +59,21 @@ class kvE_lstm_weights(C.Structure):
     _fields_ = [("W_ih", C.c_void_p), ("W_hh", C.c_void_p), ("b_ih", C.c_void_p), ("b_hh", C.c_void_p),
                 ("w_s", C.c_void_p), ("b_s", C.c_float)]
 
+
+class kvE_rope(C.Structure):
+    _fields_ = [("n_axes", C.c_int32), ("layout", C.c_int32), ("axis", C.c_uint8 * 64), ("inv_freq", C.c_double * 64)]
+
+
+class kvE_rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride_b", C.c_int64), ("stride_t", C.c_int64), ("stride_h", C.c_int64)]
+
+
+class kvE_q4_buffers(C.Structure):
+    _fields_ = [("k4_pages", C.c_void_p), ("v4_pages", C.c_void_p), ("n_pages4", C.c_int64), ("page_table4", C.c_void_p),
+                ("max_query_tokens", C.c_int32), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
+Q4_UNIT_ROWS, Q4_UNIT_BYTES = 16, 1152
 
 _lib = None
 _bind = None
@@ -125,11 +141,22 @@ def load_library(build_if_missing: bool = True) -> C.CDLL:
     lib.kvE_profile.argtypes = [C.c_void_p, C.c_int]
     lib.kvE_profile_read.argtypes = [C.c_void_p, C.POINTER(C.c_float)]
     lib.kvE_selftest_timeout.argtypes = [C.c_void_p, C.c_int, C.c_void_p]
+    lib.kvE_append_rope.argtypes = [C.c_void_p, C.c_int, C.POINTER(kvE_rows), C.POINTER(kvE_rows), C.POINTER(kvE_rows), C.c_void_p, C.c_int,
+                                    C.POINTER(kvE_rope), C.c_void_p, C.POINTER(C.c_int), C.c_void_p]
+    lib.kvE_append_rope_next.argtypes = [C.c_void_p, C.c_int, C.POINTER(kvE_rows), C.POINTER(kvE_rows), C.POINTER(kvE_rows), C.c_void_p, C.c_int,
+                                         C.c_int, C.POINTER(kvE_rope), C.c_void_p, C.c_void_p]
+    lib.kvE_q4_workspace_bytes.restype = C.c_size_t
+    lib.kvE_q4_workspace_bytes.argtypes = [C.POINTER(kvE_config), C.c_int]
+    lib.kvE_attach_q4.argtypes = [C.c_void_p, C.POINTER(kvE_q4_buffers)]
+    lib.kvE_pack_chunks.argtypes = [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p]
+    lib.kvE_unpack_chunks.argtypes = [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p]
+    lib.kvE_packed_chunks.argtypes = [C.c_void_p, C.c_int, C.POINTER(C.c_int)]
+    lib.kvE_decode_attn_q4.argtypes = lib.kvE_decode_attn_block.argtypes
     lib.kvE_last_cuda_error.restype = C.c_char_p
     lib.kvE_last_cuda_error.argtypes = [C.c_void_p]
     for name in EXPORTS:
         fn = getattr(lib, name)
-        if name not in ("kvE_workspace_bytes", "kvE_last_cuda_error"):
+        if name not in ("kvE_workspace_bytes", "kvE_q4_workspace_bytes", "kvE_last_cuda_error"):
             fn.restype = C.c_int
     _lib = lib
     return lib
@@ -203,6 +230,30 @@ class LstmWeights:
 
     def set_b_s(self, b_s: float):
         self.c.b_s = float(b_s)
+
+
+ROPE_LAYOUT = {"halves": 0, "adjacent": 1}
+
+
+class Rope:
+    """Rotary positions: sections[a] of the 64 pairs follow axis a, in order (they add up to 64 or less; the rest is not turned), with
+    the frequencies theta^(-2 j / 128) of pair j, or inv_freq[j] radians per position.  `axis` (64 axis numbers) in place of `sections` deals
+    the pairs out in any other way.  layout: pair j is (j, j + 64) ("halves") or (2 j, 2 j + 1) ("adjacent")."""
+
+    def __init__(self, sections=(64,), theta=10000.0, layout="halves", inv_freq=None, axis=None):
+        freq = [float(theta) ** (-2.0 * j / 128.0) for j in range(64)] if inv_freq is None else [float(f) for f in inv_freq]
+        if axis is None:
+            axis = [a for a, n in enumerate(sections) for _ in range(int(n))]
+            if len(axis) > 64:
+                raise ValueError(f"sections {tuple(sections)} have {len(axis)} pairs, a row has 64")
+            freq = freq[:len(axis)] + [0.0] * (64 - len(axis))
+            axis = axis + [0] * (64 - len(axis))
+            self.n_axes = len(sections)
+        else:
+            self.n_axes = max(axis) + 1
+        if len(axis) != 64 or len(freq) != 64 or min(axis) < 0 or not 1 <= self.n_axes <= 4:
+            raise ValueError("64 pairs, 1 to 4 axes")
+        self.c = kvE_rope(n_axes=self.n_axes, layout=ROPE_LAYOUT[layout], axis=(C.c_uint8 * 64)(*axis), inv_freq=(C.c_double * 64)(*freq))
 
 
 class Store:
@@ -371,6 +422,52 @@ class Store:
                          from_scratch=False, stream=None, wait=True):
         kvE_decode_step_host(self, layer, k_new, v_new, q, out, agg_weights, lstm_weights, tau, scale, from_scratch, stream, wait)
 
+    def append_rope(self, layer, q, k_new, v_new, rope, positions=None, q_out=None, stream=None):
+        """kvE_append with rotary positions turned into q and k.  Returns (q_out, chunks ready to gate)"""
+        return kvE_append_rope(self, layer, q, k_new, v_new, rope, positions, q_out, stream)
+
+    def append_rope_next(self, layer, q, k_new, v_new, rope, positions=None, q_out=None, n_reserve=0, stream=None):
+        """the same at the device-held length (graph-replayable).  Returns q_out"""
+        return kvE_append_rope_next(self, layer, q, k_new, v_new, rope, positions, q_out, n_reserve, stream)
+
+    def attach_q4(self, max_query_tokens=1, page_perm=None, seed=0):
+        """Allocates 4-bit pages for every chunk and gives them to the handle (page_perm as in the constructor)."""
+        if self.C % Q4_UNIT_ROWS:
+            raise KveError("kvE_attach_q4", -2, "chunks in 4 bits need a chunk size that is a multiple of 16")
+        n_pages = self.n_layers * self.S * self.max_chunks
+        ws_bytes = int(self.lib.kvE_q4_workspace_bytes(C.byref(self.cfg), int(max_query_tokens)))
+        if ws_bytes == 0:
+            raise KveError("kvE_q4_workspace_bytes", -2, "unsupported geometry")
+        page_bytes = self.C // Q4_UNIT_ROWS * Q4_UNIT_BYTES
+        k4, v4 = (torch.zeros((n_pages, page_bytes), dtype=torch.uint8, device=self.device) for _ in range(2))
+        if page_perm is None:
+            pt = np.arange(n_pages, dtype=np.int32)
+        elif isinstance(page_perm, str) and page_perm == "random":
+            pt = np.random.default_rng(seed).permutation(n_pages).astype(np.int32)
+        else:
+            pt = np.asarray(page_perm, np.int32)
+        table = torch.from_numpy(pt.reshape(self.n_layers, self.S, self.max_chunks).copy()).to(self.device)
+        workspace = torch.zeros((ws_bytes + 256,), dtype=torch.uint8, device=self.device)
+        buf = kvE_q4_buffers(k4_pages=k4.data_ptr(), v4_pages=v4.data_ptr(), n_pages4=n_pages, page_table4=table.data_ptr(),
+                             max_query_tokens=int(max_query_tokens), workspace=(workspace.data_ptr() + 255) // 256 * 256, workspace_bytes=ws_bytes)
+        _check("kvE_attach_q4", self.lib.kvE_attach_q4(self.handle, C.byref(buf)), self.handle)
+        self.k4_pages, self.v4_pages, self.page_table4, self.q4_workspace = k4, v4, table, workspace
+
+    def pack_chunks(self, layer, chunk_begin, chunk_end, stream=None):
+        """chunks outside the window to 4 bits"""
+        _check("kvE_pack_chunks", self.lib.kvE_pack_chunks(self.handle, layer, int(chunk_begin), int(chunk_end), _stream(self, stream)), self.handle)
+
+    def unpack_chunks(self, layer, chunk_begin, chunk_end, k_out=None, v_out=None, stream=None):
+        return kvE_unpack_chunks(self, layer, chunk_begin, chunk_end, k_out, v_out, stream)
+
+    def packed_chunks(self, layer=0) -> int:
+        n = C.c_int(0)
+        _check("kvE_packed_chunks", self.lib.kvE_packed_chunks(self.handle, layer, C.byref(n)))
+        return n.value
+
+    def decode_attn_q4(self, layer, q, dense=False, causal=False, out=None, lse=None, scale=None, stream=None):
+        return kvE_decode_attn_q4(self, layer, q, dense, causal, out, lse, scale, stream)
+
     def poll_status(self) -> int:
         return kvE_poll_status(self)
 
@@ -459,7 +556,73 @@ def kvE_decode_attn_block(st: Store, layer, q, dense=False, out=None, lse=None, 
     return out
 
 
-RECLAIM = {"discarded": 0, "gated": 1}
+def _strided_rows(st, t, heads) -> kvE_rows:
+    """a bf16 device tensor [B, n, heads, 128] with contiguous rows, of any strides"""
+    assert t.dtype is _BF16 and t.dim() == 4 and t.shape[0] == st.B and t.shape[2:] == (heads, 128) and t.stride(3) == 1
+    assert t.is_cuda and t.device.index == st.device_index
+    return kvE_rows(t.data_ptr(), *(stride if size > 1 else 0 for stride, size in zip(t.stride()[:3], t.shape)))
+
+
+def _rope_arguments(st, q, k_new, v_new, rope, positions, q_out):
+    n = k_new.shape[1]
+    k, v = _strided_rows(st, k_new, st.H), _strided_rows(st, v_new, st.H)
+    assert v_new.shape[1] == n and (q is not None or q_out is None)
+    rows = None
+    if q is not None:
+        rows = _strided_rows(st, q, st.Hq)
+        assert q.shape[1] == n
+        if q_out is None:
+            q_out = torch.empty((st.B, n, st.Hq, 128), dtype=_BF16, device=q.device)
+        assert q_out.dtype is _BF16 and q_out.shape == (st.B, n, st.Hq, 128)
+    if positions is not None:
+        assert positions.dtype == torch.int32 and positions.shape == (st.B, n, rope.n_axes)
+    return (None if rows is None else C.byref(rows)), C.byref(k), C.byref(v), _p(positions), n, q_out
+
+
+def kvE_append_rope(st: Store, layer, q, k_new, v_new, rope, positions=None, q_out=None, stream=None):
+    """q: bf16 [B, n_new, Hq, 128] or None; k_new, v_new: bf16 [B, n_new, Hkv, 128]; rows contiguous, otherwise any strides (parts of
+    one projection's output).  positions: int32 [B, n_new, n_axes], or None: the index in the cache on every axis.
+    Returns (q_out, number of chunks ready to gate)."""
+    rows, k, v, pos, n, q_out = _rope_arguments(st, q, k_new, v_new, rope, positions, q_out)
+    ready = C.c_int(0)
+    _check("kvE_append_rope", st.lib.kvE_append_rope(st.handle, layer, rows, k, v, pos, n, C.byref(rope.c), _p(q_out), C.byref(ready), _stream(st, stream)),
+           st.handle)
+    return q_out, ready.value
+
+
+def kvE_append_rope_next(st: Store, layer, q, k_new, v_new, rope, positions=None, q_out=None, n_reserve=0, stream=None):
+    rows, k, v, pos, n, q_out = _rope_arguments(st, q, k_new, v_new, rope, positions, q_out)
+    _check("kvE_append_rope_next", st.lib.kvE_append_rope_next(st.handle, layer, rows, k, v, pos, n, int(n_reserve), C.byref(rope.c), _p(q_out),
+                                                               _stream(st, stream)), st.handle)
+    return q_out
+
+
+def kvE_unpack_chunks(st: Store, layer, chunk_begin, chunk_end, k_out=None, v_out=None, stream=None):
+    """What the packed chunks stand for: bf16 [S, (chunk_end - chunk_begin) C, 128], keys and values."""
+    shape = (st.S, max(0, int(chunk_end) - int(chunk_begin)) * st.C, 128)
+    k_out, v_out = (torch.empty(shape, dtype=_BF16, device=st.device) if t is None else t for t in (k_out, v_out))
+    if shape[1] > 0:      # (an empty tensor has no address)
+        _check("kvE_unpack_chunks", st.lib.kvE_unpack_chunks(st.handle, layer, int(chunk_begin), int(chunk_end), _rows(k_out, shape), _rows(v_out, shape),
+                                                             _stream(st, stream)), st.handle)
+    return k_out, v_out
+
+
+def kvE_decode_attn_q4(st: Store, layer, q, dense=False, causal=False, out=None, lse=None, scale=None, stream=None):
+    """q: bf16 [B, T, Hq, 128] device tensor.  Returns out (same shape); lse, if given, is an fp32 [B, T, Hq] device tensor."""
+    assert q.dtype is _BF16 and q.dim() == 4 and q.shape[0] == st.B and q.shape[2:] == (st.Hq, 128)
+    if out is None:
+        out = torch.empty_like(q)
+    assert out.shape == q.shape and out.dtype is _BF16
+    if lse is not None:
+        assert lse.dtype == torch.float32 and lse.shape == q.shape[:3]
+    rc = st.lib.kvE_decode_attn_q4(st.handle, layer, _p(q), q.shape[1], 1 if dense else 0, 1 if causal else 0, _p(out), _p(lse),
+                                   _DEFAULT_SCALE if scale is None else scale, _stream(st, stream))
+    if rc:
+        _check("kvE_decode_attn_q4", rc, st.handle)
+    return out
+
+
+RECLAIM = {"discarded": 0, "gated": 1, "packed": 2}
 
 
 def kvE_reclaim_pages(st: Store, layer, chunk_begin, chunk_end, mode="discarded", free_list=None, free_count=None, stream=None):

@@ -19,6 +19,7 @@ struct LayerState {
   int n_compacted = 0;   // keep list covers chunks [0, n_compacted); attention reads raw rows from there on
   float tau = 0.f;       // threshold of the last kvE_compact
   bool by_topk = false;  // the keep list came from kvE_compact_topk (no threshold to tell "discarded" by)
+  int n_packed = 0;      // chunks [0, n_packed) have a copy in 4 bits
 };
 
 struct kvE_store {
@@ -38,6 +39,10 @@ struct kvE_store {
   int block_hp = 0, block_split_cap = 1;
   std::vector<LayerState> layers;
   std::string cuda_error;
+
+  // the 4-bit pages (kvE_attach_q4): none until then
+  kvE_q4_buffers q4 = {};
+  bool q4_ready = false;
 
   // optional per-kernel timing: one (start, stop) event pair per kernel id
   bool profiling = false;
@@ -176,6 +181,7 @@ LayerView view(const kvE_store* st, int layer) {
   v.status = b.status_word;
   v.n_listed = reinterpret_cast<int32_t*>(static_cast<char*>(b.workspace) + st->off_listed) + layer;
   v.step_ticket = v.n_listed + st->cfg.n_layers;
+  v.n_packed = st->q4_ready ? static_cast<int32_t*>(st->q4.workspace) + layer : nullptr;
   v.B = c.B; v.H = c.Hkv; v.S = st->S; v.C = c.C; v.max_chunks = st->max_chunks; v.max_tokens = c.max_tokens;
   return v;
 }
@@ -406,8 +412,11 @@ int kvE_set_len(kvE_store* st, int layer, int n, void* stream) {
   LayerState& ls = st->layers[layer];
   const int nc = stale_chunks(st->cfg, n);
   // a keep list that reaches past the new stale range is dropped, on the device too (-1: leave the device's count alone)
-  cudaError_t e = launch_set_len(view(st, layer), n, ls.n_compacted > nc ? 0 : -1, static_cast<cudaStream_t>(stream));
+  // chunks that are no longer complete lose their 4-bit copy: other rows may take their place
+  const int complete = n / st->cfg.C, packed = ls.n_packed > complete ? complete : -1;
+  cudaError_t e = launch_set_len(view(st, layer), n, ls.n_compacted > nc ? 0 : -1, packed, static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return cuda_fail(st, e);
+  if (packed >= 0) ls.n_packed = packed;
   ls.n_tokens = n;
   ls.reserve_upper = 0;
   if (ls.n_summarised > nc) ls.n_summarised = nc;
@@ -662,9 +671,9 @@ int kvE_reclaim_pages(kvE_store* st, int layer, int chunk_begin, int chunk_end, 
   if (bad_layer(st, layer) || chunk_begin < 0 || chunk_end < chunk_begin || !free_list || !free_count || capacity < 0)
     return KVE_ERR_ARG;
   if (wrong_device(st)) return KVE_ERR_STATE;
-  if (mode != KVE_RECLAIM_DISCARDED && mode != KVE_RECLAIM_GATED) return KVE_ERR_ARG;
+  if (mode != KVE_RECLAIM_DISCARDED && mode != KVE_RECLAIM_GATED && mode != KVE_RECLAIM_PACKED) return KVE_ERR_ARG;
   const LayerState& ls = st->layers[layer];
-  if (chunk_end > ls.n_compacted) return KVE_ERR_STATE;                        // only chunks the retention rule has judged
+  if (chunk_end > (mode == KVE_RECLAIM_PACKED ? ls.n_packed : ls.n_compacted)) return KVE_ERR_STATE;      // only chunks the retention rule has judged, or that are held in 4 bits
   if (mode == KVE_RECLAIM_GATED && st->cfg.attend != KVE_ATTEND_SUMMARY) return KVE_ERR_STATE;   // RAW attention still reads kept pages
   if (mode == KVE_RECLAIM_DISCARDED && ls.by_topk) return KVE_ERR_STATE;       // "discarded" is defined by the threshold rule
   if (chunk_end == chunk_begin) {
@@ -672,7 +681,7 @@ int kvE_reclaim_pages(kvE_store* st, int layer, int chunk_begin, int chunk_end, 
     return e == cudaSuccess ? KVE_OK : cuda_fail(st, e);
   }
   int32_t* scratch = reinterpret_cast<int32_t*>(static_cast<char*>(st->buf.workspace) + st->off_reclaim);
-  cudaError_t e = launch_reclaim(view(st, layer), chunk_begin, chunk_end, ls.tau, mode, scratch, free_list, capacity, free_count,
+  cudaError_t e = launch_reclaim(view(st, layer), chunk_begin, chunk_end, ls.tau, mode == KVE_RECLAIM_PACKED ? KVE_RECLAIM_GATED : mode, scratch, free_list, capacity, free_count,
                                  static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? KVE_OK : cuda_fail(st, e);
 }
@@ -877,6 +886,211 @@ int kvE_selftest_timeout(kvE_store* st, int which, void* stream) {
   if (wrong_device(st)) return KVE_ERR_STATE;
   static_assert(SELFTEST_RING_BYTES <= ATTN_GRID_LIMIT * ATTN_PARTIAL_FLOATS * sizeof(float), "what the ring reads: partial records");
   cudaError_t e = launch_selftest_timeout(which, static_cast<char*>(st->buf.workspace) + st->off_partials, st->buf.status_word, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? KVE_OK : cuda_fail(st, e);
+}
+
+}  // extern "C"
+
+// ---- rotary positions with the append ------------------------------------------------------------------------------------------
+namespace {
+
+// rows of 256 bytes that the kernel fetches 16 bytes at a time, wherever the strides put them
+bool bad_rows(const kvE_rows* r) {
+  return !r || !r->data || reinterpret_cast<uintptr_t>(r->data) % 16 != 0 || r->stride_b % 8 != 0 || r->stride_t % 8 != 0 || r->stride_h % 8 != 0;
+}
+
+int append_rope(kvE_store* st, int layer, const kvE_rows* q, const kvE_rows* k_new, const kvE_rows* v_new, const int32_t* positions, int n_new,
+                const kvE_rope* rope, void* q_out, bool next, cudaStream_t stream) {
+  const kvE_config& c = st->cfg;
+  const LayerState& ls = st->layers[layer];
+  if (rope->n_axes < 1 || rope->n_axes > KVE_ROPE_MAX_AXES || (rope->layout != KVE_ROPE_HALVES && rope->layout != KVE_ROPE_ADJACENT)) return KVE_ERR_ARG;
+  if (bad_rows(k_new) || bad_rows(v_new) || (q != nullptr) != (q_out != nullptr) || (q && bad_rows(q)) || reinterpret_cast<uintptr_t>(q_out) % 16 != 0) return KVE_ERR_ARG;
+  if ((long long)c.B * n_new * (c.Hq + 2LL * c.Hkv) > 0x7fffffffLL) return KVE_ERR_GEOMETRY;
+  RopeCall call = {};
+  auto rows = [](const kvE_rows& r) { return RopeRows{static_cast<const uint16_t*>(r.data), (long long)r.stride_b, (long long)r.stride_t, (long long)r.stride_h}; };
+  if (q) call.q = rows(*q);
+  call.k = rows(*k_new);
+  call.v = rows(*v_new);
+  for (int j = 0; j < 64; ++j) {
+    if (rope->axis[j] >= rope->n_axes) return KVE_ERR_ARG;
+    call.axis[j] = rope->axis[j];
+    call.turns[j] = rope->inv_freq[j] * 0.15915494309189533576888376337251;      // 1 / (2 pi)
+  }
+  call.positions = positions;
+  call.q_out = static_cast<uint16_t*>(q_out);
+  call.n_new = n_new; call.Hq = q ? c.Hq : 0; call.n_axes = rope->n_axes; call.adjacent = rope->layout == KVE_ROPE_ADJACENT ? 1 : 0;
+  call.pos0 = ls.n_tokens;
+  call.ticket = reinterpret_cast<int32_t*>(static_cast<char*>(st->buf.workspace) + st->off_ticket);
+  Prof prof(st, KVE_K_APPEND, stream);
+  const cudaError_t e = launch_append_rope(view(st, layer), call, next, stream);
+  return e == cudaSuccess ? KVE_OK : cuda_fail(st, e);
+}
+
+}  // namespace
+
+extern "C" {
+
+int kvE_append_rope(kvE_store* st, int layer, const kvE_rows* q, const kvE_rows* k_new, const kvE_rows* v_new, const int32_t* positions, int n_new,
+                    const kvE_rope* rope, void* q_out, int* n_ready, void* stream) {
+  if (bad_layer(st, layer) || !k_new || !v_new || !rope || n_new < 0) return KVE_ERR_ARG;
+  if (wrong_device(st)) return KVE_ERR_STATE;
+  LayerState& ls = st->layers[layer];
+  if ((long long)ls.n_tokens + n_new > st->cfg.max_tokens) return KVE_ERR_CAPACITY;
+  if (n_new > 0) {
+    const int rc = append_rope(st, layer, q, k_new, v_new, positions, n_new, rope, q_out, false, static_cast<cudaStream_t>(stream));
+    if (rc != KVE_OK) return rc;
+    ls.n_tokens += n_new;
+    ls.reserve_upper = 0;
+  }
+  if (n_ready) *n_ready = stale_chunks(st->cfg, ls.n_tokens) - ls.n_gated;
+  return KVE_OK;
+}
+
+int kvE_append_rope_next(kvE_store* st, int layer, const kvE_rows* q, const kvE_rows* k_new, const kvE_rows* v_new, const int32_t* positions, int n_new,
+                         int n_reserve, const kvE_rope* rope, void* q_out, void* stream) {
+  if (bad_layer(st, layer) || !k_new || !v_new || !rope || n_new <= 0 || n_reserve < 0) return KVE_ERR_ARG;
+  if (wrong_device(st)) return KVE_ERR_STATE;
+  LayerState& ls = st->layers[layer];
+  if ((long long)ls.n_tokens + n_new > st->cfg.max_tokens) return KVE_ERR_CAPACITY;
+  const int rc = append_rope(st, layer, q, k_new, v_new, positions, n_new, rope, q_out, true, static_cast<cudaStream_t>(stream));
+  if (rc != KVE_OK) return rc;
+  long long upper = (long long)ls.n_tokens + n_new + n_reserve;
+  if (upper > st->cfg.max_tokens) upper = st->cfg.max_tokens;
+  if (upper > ls.reserve_upper) ls.reserve_upper = (int)upper;
+  ls.n_tokens += n_new;
+  return KVE_OK;
+}
+
+}  // extern "C"
+
+// ---- the cache in 4 bits -----------------------------------------------------------------------------------------------------------
+namespace {
+
+// most parts a sequence is cut into: two CTAs per SM, twice over
+int q4_split_cap(long long S) {
+  const long long c = 4LL * sm_count() / S;
+  return (int)(c < 1 ? 1 : (c > 2LL * sm_count() ? 2LL * sm_count() : c));
+}
+struct Q4Carve { size_t off_counters, off_partials, total; };      // in front: [n_layers] chunks packed, as the device knows it
+Q4Carve q4_carve(const kvE_config& c, int max_query_tokens) {
+  const size_t S = (size_t)c.B * c.Hkv, rows = (size_t)max_query_tokens * (c.Hq / c.Hkv);
+  Q4Carve k;
+  k.off_counters = align_up((size_t)c.n_layers * sizeof(int32_t));
+  k.off_partials = align_up(k.off_counters + S * q4_attn_row_groups((int)rows) * sizeof(int32_t));
+  k.total = align_up(k.off_partials + S * q4_split_cap((long long)S) * rows * ATTN_PARTIAL_FLOATS * sizeof(float));
+  return k;
+}
+int check_q4(const kvE_config* c, int max_query_tokens) {
+  const int rc = check_config(c);
+  if (rc != KVE_OK) return rc;
+  if (max_query_tokens < 1) return KVE_ERR_ARG;
+  if (c->C % Q4_UNIT_ROWS != 0 || (long long)max_query_tokens * (c->Hq / c->Hkv) > Q4_MAX_ROWS) return KVE_ERR_GEOMETRY;
+  return KVE_OK;
+}
+Q4Pages q4_pages(const kvE_store* st, int layer) {
+  return Q4Pages{static_cast<uint8_t*>(st->q4.k4_pages), static_cast<uint8_t*>(st->q4.v4_pages), st->q4.n_pages4,
+                 st->q4.page_table4 + (size_t)layer * st->S * st->max_chunks};
+}
+
+// Into how many parts a launch cuts every sequence.
+int q4_splits(const kvE_store* st, const LayerState& ls, bool dense, int rows) {
+  const int C = st->cfg.C;
+  const long long n_upper = ls.reserve_upper > ls.n_tokens ? ls.reserve_upper : ls.n_tokens;
+  const int listed = dense ? 0 : ls.n_compacted;
+  const long long chunks4 = ls.n_packed - (listed < ls.n_packed ? listed : ls.n_packed) + (listed < ls.n_packed ? listed : ls.n_packed) / 2;      // about half of the listed ones are kept
+  const long long front = listed > ls.n_packed ? listed : ls.n_packed, late = listed > ls.n_packed ? listed - ls.n_packed : 0;
+  long long tiles = chunks4 * ((C + 31) / 32) + late / 2 * (C / 8) + (n_upper - front * C + 7) / 8;
+  if (tiles < 1) tiles = 1;
+  const int groups = q4_attn_row_groups(rows);
+  const long long slots = (rows <= 8 ? 2LL : 1LL) * sm_count();
+  const int cap = q4_split_cap(st->S);
+  double best = 1e30;
+  int pick = 1;
+  for (int k = 1; k <= cap; ++k) {
+    const long long ctas = (long long)st->S * groups * k;
+    const double waves = (double)((ctas + slots - 1) / slots);
+    const double us = waves * ((double)((tiles + k - 1) / k) * 0.2 + 2.0) + (k > 1 ? 1.5 + 0.02 * k : 0.0);
+    if (us < best - 0.05) { best = us; pick = k; }
+  }
+  return pick;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t kvE_q4_workspace_bytes(const kvE_config* cfg, int max_query_tokens) {
+  if (check_q4(cfg, max_query_tokens) != KVE_OK) return 0;
+  return q4_carve(*cfg, max_query_tokens).total;
+}
+
+int kvE_attach_q4(kvE_store* st, const kvE_q4_buffers* buf) {
+  if (!st || !buf || !buf->k4_pages || !buf->v4_pages || !buf->page_table4 || !buf->workspace || buf->n_pages4 <= 0) return KVE_ERR_ARG;
+  if (wrong_device(st)) return KVE_ERR_STATE;
+  const int rc = check_q4(&st->cfg, buf->max_query_tokens);
+  if (rc != KVE_OK) return rc;
+  for (const void* p : {buf->k4_pages, buf->v4_pages})
+    if (reinterpret_cast<uintptr_t>(p) % 16 != 0) return KVE_ERR_ARG;
+  if (reinterpret_cast<uintptr_t>(buf->workspace) % ALIGN != 0) return KVE_ERR_ARG;
+  const Q4Carve k = q4_carve(st->cfg, buf->max_query_tokens);
+  if (buf->workspace_bytes < k.total) return KVE_ERR_CAPACITY;
+  cudaError_t e = cudaDeviceSynchronize();      // (work that still uses pages attached before)
+  if (e == cudaSuccess) e = cudaMemset(buf->workspace, 0, k.off_partials);
+  if (e == cudaSuccess) e = cudaDeviceSynchronize();
+  if (e != cudaSuccess) return cuda_fail(st, e);
+  st->q4 = *buf;
+  st->q4_ready = true;
+  for (LayerState& ls : st->layers) ls.n_packed = 0;
+  return KVE_OK;
+}
+
+int kvE_pack_chunks(kvE_store* st, int layer, int chunk_begin, int chunk_end, void* stream) {
+  if (bad_layer(st, layer) || chunk_begin < 0 || chunk_end < chunk_begin) return KVE_ERR_ARG;
+  if (wrong_device(st) || !st->q4_ready) return KVE_ERR_STATE;
+  LayerState& ls = st->layers[layer];
+  if (chunk_begin > ls.n_packed || chunk_end > stale_chunks(st->cfg, ls.n_tokens)) return KVE_ERR_STATE;
+  if (chunk_end == chunk_begin) return KVE_OK;
+  Prof prof(st, KVE_K_PACK, static_cast<cudaStream_t>(stream));
+  const cudaError_t e = launch_pack(view(st, layer), q4_pages(st, layer), chunk_begin, chunk_end, chunk_end > ls.n_packed ? chunk_end : -1, static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return cuda_fail(st, e);
+  if (chunk_end > ls.n_packed) ls.n_packed = chunk_end;
+  return KVE_OK;
+}
+
+int kvE_unpack_chunks(kvE_store* st, int layer, int chunk_begin, int chunk_end, void* k_out, void* v_out, void* stream) {
+  if (bad_layer(st, layer) || chunk_begin < 0 || chunk_end < chunk_begin || !k_out || !v_out) return KVE_ERR_ARG;
+  for (const void* p : {k_out, v_out})
+    if (reinterpret_cast<uintptr_t>(p) % 16 != 0) return KVE_ERR_ARG;
+  if (wrong_device(st) || !st->q4_ready) return KVE_ERR_STATE;
+  if (chunk_end > st->layers[layer].n_packed) return KVE_ERR_STATE;
+  if (chunk_end == chunk_begin) return KVE_OK;
+  const cudaError_t e = launch_unpack(view(st, layer), q4_pages(st, layer), chunk_begin, chunk_end, k_out, v_out, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? KVE_OK : cuda_fail(st, e);
+}
+
+int kvE_packed_chunks(const kvE_store* st, int layer, int* n_packed) {
+  if (bad_layer(st, layer) || !n_packed) return KVE_ERR_ARG;
+  *n_packed = st->layers[layer].n_packed;
+  return KVE_OK;
+}
+
+int kvE_decode_attn_q4(kvE_store* st, int layer, const void* q, int n_query_tokens, int dense, int causal, void* out, float* lse, float scale,
+                       void* stream) {
+  if (bad_layer(st, layer) || !q || !out || n_query_tokens <= 0) return KVE_ERR_ARG;
+  for (const void* p : {q, (const void*)out})
+    if (reinterpret_cast<uintptr_t>(p) % 16 != 0) return KVE_ERR_ARG;
+  if (wrong_device(st) || !st->q4_ready) return KVE_ERR_STATE;
+  if (n_query_tokens > st->q4.max_query_tokens) return KVE_ERR_CAPACITY;
+  const LayerState& ls = st->layers[layer];
+  const int G = st->cfg.Hq / st->cfg.Hkv;
+  const int front = dense || ls.n_compacted < ls.n_packed ? ls.n_packed : ls.n_compacted;      // chunks in front of the raw tail
+  if (causal && (long long)ls.n_tokens - (long long)front * st->cfg.C < n_query_tokens) return KVE_ERR_STATE;
+  const Q4Carve k = q4_carve(st->cfg, st->q4.max_query_tokens);
+  char* ws = static_cast<char*>(st->q4.workspace);
+  Prof prof(st, KVE_K_ATTN_Q4, static_cast<cudaStream_t>(stream));
+  const cudaError_t e = launch_attn_q4(view(st, layer), q4_pages(st, layer), dense != 0, n_query_tokens, G, causal != 0,
+                                       q4_splits(st, ls, dense != 0, n_query_tokens * G), q, out, lse, scale,
+                                       reinterpret_cast<float*>(ws + k.off_partials), reinterpret_cast<int32_t*>(ws + k.off_counters), static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? KVE_OK : cuda_fail(st, e);
 }
 

@@ -46,6 +46,7 @@ struct LayerView {
   int32_t* status;
   int32_t* n_listed;          // one int: chunks [0, *n_listed) are covered by the keep list (device copy of the handle's count)
   int32_t* step_ticket;       // one int, zero between launches: arrivals of the gate-step kernel's clusters
+  int32_t* n_packed;          // one int: chunks [0, *n_packed) have a copy in 4 bits; null: the handle has no 4-bit pages
   int B, H, S, C, max_chunks, max_tokens;
 };
 
@@ -67,10 +68,39 @@ constexpr int ATTN_PARTIAL_FLOATS = 132;       // acc[128], m, l, 2 pad: keeps e
 // q_src, q_dst: S rows to copy along, or null
 cudaError_t launch_append(const LayerView& v, const void* k_new, const void* v_new, int n_new, int pos0, cudaStream_t st,
                           const void* q_src = nullptr, void* q_dst = nullptr);
-// n_listed >= 0: also set the device copy of the keep list's coverage to it
-cudaError_t launch_set_len(const LayerView& v, int n, int n_listed, cudaStream_t st);
+// n_listed >= 0: also set the device copy of the keep list's coverage to it; n_packed >= 0: that of the 4-bit chunks
+cudaError_t launch_set_len(const LayerView& v, int n, int n_listed, int n_packed, cudaStream_t st);
 cudaError_t launch_append_next(const LayerView& v, const void* k_new, const void* v_new, int n_new, int32_t* ticket,
                                cudaStream_t st);
+// q, k and v as they come: strides in elements over batch, token and head
+struct RopeRows { const uint16_t* data; long long stride_b, stride_t, stride_h; };
+struct RopeCall {
+  RopeRows q, k, v;
+  const int32_t* positions;   // [B][n_new][n_axes], or null: the index in the cache on every axis
+  uint16_t* q_out;            // [B][n_new][Hq][128], or null: no q
+  int n_new, Hq, n_axes, adjacent;
+  int pos0;                   // tokens stored before (not read by the form that takes it from the device)
+  int32_t* ticket;            // that form's last-CTA ticket
+  double turns[64];           // whole turns per position of every pair
+  uint8_t axis[64];           // the axis whose position turns it
+};
+cudaError_t launch_append_rope(const LayerView& v, const RopeCall& call, bool next, cudaStream_t st);
+
+// the cache in 4 bits (layout: q4.cuh)
+struct Q4Pages {
+  uint8_t *k, *v;             // [n_pages][C / 16][Q4_UNIT_BYTES]
+  long long n_pages;
+  const int32_t* table;       // [S][max_chunks], this layer's
+};
+constexpr int Q4_UNIT_ROWS = 16, Q4_UNIT_BYTES = 1152;
+cudaError_t launch_pack(const LayerView& v, const Q4Pages& p, int t0, int t1, int n_packed, cudaStream_t st);
+cudaError_t launch_unpack(const LayerView& v, const Q4Pages& p, int t0, int t1, void* k_out, void* v_out, cudaStream_t st);
+// attention of T query tokens on G query heads a KV head; splits: equal parts every sequence is cut into;
+// partials: [S][splits][T G] records of ATTN_PARTIAL_FLOATS; counters: [query groups][S], zero between launches
+constexpr int Q4_MAX_ROWS = 128;
+int q4_attn_row_groups(int rows);      // groups of query rows that CTAs of their own take
+cudaError_t launch_attn_q4(const LayerView& v, const Q4Pages& p, bool dense, int T, int G, bool causal, int splits, const void* q, void* out, float* lse,
+                           float scale, float* partials, int32_t* counters, cudaStream_t st);
 // dev_window < 0: chunks [t0, t1).  dev_window >= 0 (the window size W): ONE chunk per sequence whose index the kernel
 // finds on the device - the chunk behind the keep list's coverage, if the stored length says it has left the window,
 // else the launch does nothing (a trigger that is replayed from a CUDA graph)
