@@ -966,18 +966,21 @@ int kvE_append_rope_next(kvE_store* st, int layer, const kvE_rows* q, const kvE_
 // ---- the cache in 4 bits -----------------------------------------------------------------------------------------------------------
 namespace {
 
-// most parts a sequence is cut into: two CTAs per SM, twice over
-int q4_split_cap(long long S) {
-  const long long c = 4LL * sm_count() / S;
-  return (int)(c < 1 ? 1 : (c > 2LL * sm_count() ? 2LL * sm_count() : c));
-}
 struct Q4Carve { size_t off_counters, off_partials, total; };      // in front: [n_layers] chunks packed, as the device knows it
 Q4Carve q4_carve(const kvE_config& c, int max_query_tokens) {
-  const size_t S = (size_t)c.B * c.Hkv, rows = (size_t)max_query_tokens * (c.Hq / c.Hkv);
+  const size_t S = (size_t)c.B * c.Hkv;
+  const int most = max_query_tokens * (c.Hq / c.Hkv);
+  size_t items = 0, records = 0;      // over all numbers of query rows that a call may come with
+  for (int rows = 1; rows <= most; ++rows) {
+    const Q4AttnShape sh = q4_attn_shape(rows);
+    const size_t n = S * sh.groups, r = (S + (size_t)sm_count()) * sh.groups * sh.cols;
+    if (n > items) items = n;
+    if (r > records) records = r;
+  }
   Q4Carve k;
   k.off_counters = align_up((size_t)c.n_layers * sizeof(int32_t));
-  k.off_partials = align_up(k.off_counters + S * q4_attn_row_groups((int)rows) * sizeof(int32_t));
-  k.total = align_up(k.off_partials + S * q4_split_cap((long long)S) * rows * ATTN_PARTIAL_FLOATS * sizeof(float));
+  k.off_partials = align_up(k.off_counters + items * sizeof(int32_t));
+  k.total = align_up(k.off_partials + records * ATTN_PARTIAL_FLOATS * sizeof(float));
   return k;
 }
 int check_q4(const kvE_config* c, int max_query_tokens) {
@@ -992,27 +995,39 @@ Q4Pages q4_pages(const kvE_store* st, int layer) {
                  st->q4.page_table4 + (size_t)layer * st->S * st->max_chunks};
 }
 
-// Into how many parts a launch cuts every sequence.
-int q4_splits(const kvE_store* st, const LayerState& ls, bool dense, int rows) {
+// How an attention launch is cut up: every sequence into k equal parts, `runs` CTAs (for every group of query rows) with a contiguous run of them each.
+// The cheaper of two ways, in microseconds: a number of CTAs of its own for every sequence, or one resident wave that goes from sequence to sequence, which costs
+// a CTA 3 us a turn (state to shared memory, another's query rows, a first tile that raises every reference) and 2.5 us where records meet.
+// Measured (graph of launches): 8 sequences of 100003 rows, 4 query rows: 16 CTAs each 34.4 us, 148 CTAs in a wave 35.7, 8 each 52.8; 64 of 4099: 2 each 19.7, wave 22.3 to
+// 26.8; 128 of 4167, half kept: 1 each 19.4, wave 23.7; 512 of 16512, half kept: wave of halves 170, of fifths 178, of whole sequences 191.
+struct Q4Cut { int k, runs; };
+Q4Cut q4_cut(const kvE_store* st, const LayerState& ls, bool dense, int rows) {
   const int C = st->cfg.C;
   const long long n_upper = ls.reserve_upper > ls.n_tokens ? ls.reserve_upper : ls.n_tokens;
-  const int listed = dense ? 0 : ls.n_compacted;
-  const long long chunks4 = ls.n_packed - (listed < ls.n_packed ? listed : ls.n_packed) + (listed < ls.n_packed ? listed : ls.n_packed) / 2;      // about half of the listed ones are kept
-  const long long front = listed > ls.n_packed ? listed : ls.n_packed, late = listed > ls.n_packed ? listed - ls.n_packed : 0;
-  long long tiles = chunks4 * ((C + 31) / 32) + late / 2 * (C / 8) + (n_upper - front * C + 7) / 8;
+  const long long listed = dense ? 0 : ls.n_compacted, packed = ls.n_packed, front = listed > packed ? listed : packed;
+  // tiles of a sequence; about half of the listed chunks are kept
+  const long long chunks4 = listed < packed ? packed - listed + listed / 2 : packed / 2, chunks16 = listed < packed ? 0 : (listed - packed) / 2;
+  long long tiles = chunks4 * ((C + 31) / 32) + chunks16 * (C / 8) + (n_upper - front * C + 7) / 8;
   if (tiles < 1) tiles = 1;
-  const int groups = q4_attn_row_groups(rows);
-  const long long slots = (rows <= 8 ? 2LL : 1LL) * sm_count();
-  const int cap = q4_split_cap(st->S);
+  const Q4AttnShape shape = q4_attn_shape(rows);
+  const long long S = st->S, most = sm_count() / shape.groups > 1 ? sm_count() / shape.groups : 1;
+  const double tile_us = shape.cols <= 8 ? 0.138 : 0.24, join_us = 2.5, turn_us = 3.0;
+  long long runs = S, k = 1;
   double best = 1e30;
-  int pick = 1;
-  for (int k = 1; k <= cap; ++k) {
-    const long long ctas = (long long)st->S * groups * k;
-    const double waves = (double)((ctas + slots - 1) / slots);
-    const double us = waves * ((double)((tiles + k - 1) / k) * 0.2 + 2.0) + (k > 1 ? 1.5 + 0.02 * k : 0.0);
-    if (us < best - 0.05) { best = us; pick = k; }
+  // m CTAs for every sequence, which stay with it
+  for (long long m = 1; m * S <= most && m <= tiles; ++m) {
+    const double us = (double)((tiles + m - 1) / m) * tile_us + (m > 1 ? join_us + 0.05 * (double)m : 0.0);
+    if (us < best) { best = us; runs = m * S; k = m; }
   }
-  return pick;
+  // one resident wave, whose CTAs go from one sequence to the next
+  for (long long kk = 1; kk <= 16 && kk <= tiles && S * kk > most; ++kk) {
+    const long long parts = (S * kk + most - 1) / most;
+    const double us = (double)parts / (double)kk * (double)tiles * tile_us + turn_us * (double)((parts + kk - 1) / kk - (kk == 1 ? 1 : 0)) + (kk > 1 ? join_us : 0.0);
+    if (us < best) { best = us; runs = most; k = kk; }
+  }
+  while (k > 1 && S * k * (runs + 1) >= (1LL << 31)) --k;      // the kernel's arithmetic
+  if (runs > S * k) runs = S * k;
+  return Q4Cut{(int)k, (int)runs};
 }
 
 }  // namespace
@@ -1088,8 +1103,8 @@ int kvE_decode_attn_q4(kvE_store* st, int layer, const void* q, int n_query_toke
   const Q4Carve k = q4_carve(st->cfg, st->q4.max_query_tokens);
   char* ws = static_cast<char*>(st->q4.workspace);
   Prof prof(st, KVE_K_ATTN_Q4, static_cast<cudaStream_t>(stream));
-  const cudaError_t e = launch_attn_q4(view(st, layer), q4_pages(st, layer), dense != 0, n_query_tokens, G, causal != 0,
-                                       q4_splits(st, ls, dense != 0, n_query_tokens * G), q, out, lse, scale,
+  const Q4Cut cut = q4_cut(st, ls, dense != 0, n_query_tokens * G);
+  const cudaError_t e = launch_attn_q4(view(st, layer), q4_pages(st, layer), dense != 0, n_query_tokens, G, causal != 0, cut.k, cut.runs, q, out, lse, scale,
                                        reinterpret_cast<float*>(ws + k.off_partials), reinterpret_cast<int32_t*>(ws + k.off_counters), static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? KVE_OK : cuda_fail(st, e);
 }

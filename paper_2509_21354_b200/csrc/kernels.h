@@ -95,12 +95,13 @@ struct Q4Pages {
 constexpr int Q4_UNIT_ROWS = 16, Q4_UNIT_BYTES = 1152;
 cudaError_t launch_pack(const LayerView& v, const Q4Pages& p, int t0, int t1, int n_packed, cudaStream_t st);
 cudaError_t launch_unpack(const LayerView& v, const Q4Pages& p, int t0, int t1, void* k_out, void* v_out, cudaStream_t st);
-// attention of T query tokens on G query heads a KV head; splits: equal parts every sequence is cut into;
-// partials: [S][splits][T G] records of ATTN_PARTIAL_FLOATS; counters: [query groups][S], zero between launches
+// attention of T query tokens on G query heads a KV head.  Query rows go in `groups` of `cols`, one CTA each; every sequence is cut into parts_per_seq equal
+// parts, and `runs` CTAs per group share them; partials: (S + runs) groups records of `cols` rows of ATTN_PARTIAL_FLOATS; counters: S groups, zero between launches
 constexpr int Q4_MAX_ROWS = 128;
-int q4_attn_row_groups(int rows);      // groups of query rows that CTAs of their own take
-cudaError_t launch_attn_q4(const LayerView& v, const Q4Pages& p, bool dense, int T, int G, bool causal, int splits, const void* q, void* out, float* lse,
-                           float scale, float* partials, int32_t* counters, cudaStream_t st);
+struct Q4AttnShape { int cols, groups; };
+Q4AttnShape q4_attn_shape(int rows);
+cudaError_t launch_attn_q4(const LayerView& v, const Q4Pages& p, bool dense, int T, int G, bool causal, int parts_per_seq, int runs, const void* q, void* out,
+                           float* lse, float scale, float* partials, int32_t* counters, cudaStream_t st);
 // dev_window < 0: chunks [t0, t1).  dev_window >= 0 (the window size W): ONE chunk per sequence whose index the kernel
 // finds on the device - the chunk behind the keep list's coverage, if the stored length says it has left the window,
 // else the launch does nothing (a trigger that is replayed from a CUDA graph)

@@ -6,7 +6,8 @@
 //
 // Pages are made of units of 16 rows, 1152 bytes: 1024 of codes in the order in which a warp's lanes feed them to m16n8k16 MMAs, then
 // [16 rows][2 groups] pairs (s, low) of bf16.  A 32-bit word holds eight codes as four pairs: pair e in the bits 4 e .. 4 e + 3 of both
-// halves, the whole turned left by 3, so that one mask puts a pair into the top mantissa bits of two bf16 numbers: 0x3f80 | c << 3 is 1 + c / 16.
+// halves.  As the bits of an fp16 number a code c by itself is c 2^-24, and c << 4 is c 2^-20 (numbers without a leading one, which the tensor
+// cores take as exactly as others): two masks and a shift by 8 make four operand registers of a word.
 //   keys:   word (row, t, j) at row * 64 + t * 16 + j * 4: the numbers 32 j + 8 t .. + 7 of the row, pair e = numbers 2 e, 2 e + 1
 //           (lane (row, t) of the first MMA operand; the contraction runs over the numbers in any order that q shares)
 //   values: word (h, lane, m) at h * 512 + lane * 16 + m * 4, lane = 4 g + t: numbers d = 64 h + 8 g + 2 m and d + 1 of four rows;
@@ -20,16 +21,14 @@ namespace kve {
 constexpr int Q4_CODE_BYTES = Q4_UNIT_ROWS * D / 2;      // of a unit: 1024
 static_assert(Q4_UNIT_BYTES == Q4_CODE_BYTES + Q4_UNIT_ROWS * 2 * 4, "codes, then a scale and a lowest number for two groups of each row");
 
-// the bf16 pairs 1 + c / 16 of a word's four pairs
+// the four pairs of a word as fp16 numbers: c 2^-24, c 2^-20, c 2^-24, c 2^-20
 __device__ __forceinline__ void q4_spread(uint32_t w, uint32_t (&pair)[4]) {
-  constexpr uint32_t MASK = 0x00780078u, ONE = 0x3f803f80u;
-  pair[0] = (w & MASK) | ONE;
-  pair[1] = ((w >> 4) & MASK) | ONE;
-  pair[2] = ((w >> 8) & MASK) | ONE;
-  pair[3] = (__funnelshift_r(w, w, 12) & MASK) | ONE;
+  const uint32_t x = w >> 8;
+  pair[0] = w & 0x000f000fu;
+  pair[1] = w & 0x00f000f0u;
+  pair[2] = x & 0x000f000fu;
+  pair[3] = x & 0x00f000f0u;
 }
-__device__ __forceinline__ uint32_t q4_turn(uint32_t natural) { return __funnelshift_l(natural, natural, 3); }
-__device__ __forceinline__ uint32_t q4_unturn(uint32_t word) { return __funnelshift_r(word, word, 3); }
 
 // 4 x 4 bytes: byte m of w[i] becomes byte i of w[m]
 __device__ __forceinline__ void transpose_bytes(uint32_t (&w)[4]) {

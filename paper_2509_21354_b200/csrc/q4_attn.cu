@@ -5,547 +5,810 @@
 // HBM is the floor: 144 bytes a packed row, 512 a bf16 row, each read once per group of query rows.  At 144 bytes a row the SM has ~100
 // cycles for 16 rows, so what has to be small is the number of instructions per code:
 //  * the codes lie in the pages in the order of the MMA operands (q4.cuh): eight of them are one 32-bit word of one lane, and become four
-//    operand registers in seven instructions.  They enter the products as 1 + c / 16, exactly; scale and lowest number of a group
-//    are applied to the sums (keys: per row and group to the logit) or to the weights (values: p s per group of 64 dims).
+//    operand registers (fp16 numbers c 2^-24 and c 2^-20) in five logic instructions.  The powers of two go into q, into the softmax's scale and into
+//    the result; scale and lowest number of a group are applied to the sums (keys: per row and group to the logit) or to the weights (values:
+//    p s per group of 64 dims).  q enters as fp16 as well, times a power of two that puts its largest number at 2^14: exact but for numbers 2^25 below that.
 //  * both products are m16n8k16 MMAs with the cache on the M side (keys: 16 rows; values, transposed: 16 dims) and the queries in the
-//    eight columns.  The weights p s enter as two bf16 planes (16 bits); with up to four query rows the planes take four columns each
-//    and cost one MMA.  The logits' accumulator becomes the weights' operand through movmatrix, in registers.
-//  * a warp is on its own: it has a ring of stages in shared memory, asks for its tiles by bulk copies (one lane), waits for them and
-//    keeps its softmax state in registers.  No barrier between warps before the end.  A tile is 32 packed rows or 8 bf16 rows: about as many
-//    bytes, so that equal counts are equal work.
+//    eight columns.  The logits' accumulator becomes the weights' operand through movmatrix, in registers.
+//  * the weights p s F of packed rows are fp16: 11 bits, whose rounding (2^-12 a row) stays far below the result's own (2^-9).  F, a power of two per
+//    warp and group, follows the largest p s so that they neither overflow nor run out of bits.  bf16 rows take their weights as two bf16 planes.
+//  * a tile's products with the values are summed from zero and added to the accumulator by ordinary additions: the tensor core cuts off what lies below
+//    the last bit of its accumulator at every step, always in one direction.
 //  * the reference of the softmax is raised only when a logit passes it by more than 2^8 (a vote), not at every tile.
-// A sequence's tiles are cut into `splits` equal parts, a CTA each; the last CTA of a sequence to finish merges the records.
+//  * a consumer warp is on its own: a ring of stages and a softmax state in registers for the whole sequence.  A tile is 32 packed rows or 8 bf16 rows: about as
+//    many bytes, so that equal counts are equal work.  Two producer warps ask for all of them, a lane per consumer (done by the consumers themselves that was a
+//    sixth of all instructions); a planner warp looks them up ahead, 32 side by side, into a table in shared memory.
+//  * every sequence is cut into k equal parts, and a CTA of one resident wave takes a contiguous run of them: all CTAs have about the same number of
+//    tiles, whatever the sequences.  At the end of a sequence a consumer leaves its state in shared memory and goes on; the merger warp folds the states.
+// More than 16 query rows: groups of 16 in neighbouring CTAs, which go through the same rows at the same time (HBM reads them once).
+// A CTA with a whole sequence writes the result, others a record; the last CTA of a sequence to finish merges the records.
+// Every wait is bounded; on give-up the status word gets KVE_ERR_TIMEOUT.
+#include <type_traits>
+
 #include "q4.cuh"
 
 namespace kve {
 
-constexpr int QA_WARPS = 8;
 constexpr int QA_TILE_BYTES = 4 * Q4_UNIT_BYTES;             // two units of keys, two of values
 constexpr int QA_V_OFF = 2 * Q4_UNIT_BYTES;                  // values behind the keys
 constexpr int QA_ROWS4 = 2 * Q4_UNIT_ROWS, QA_ROWS16 = 8;    // rows of a tile of either kind
-// bf16 rows are spread out in the stage so that the lanes' reads meet different banks
-__device__ __forceinline__ constexpr int qa_k_row(int r) { return (r >> 1) * 576 + (r & 1) * 320; }
-__device__ __forceinline__ constexpr int qa_v_row(int r) { return QA_V_OFF + r * 272; }
-static_assert(qa_k_row(7) + ROW_BYTES <= QA_V_OFF && qa_v_row(7) + ROW_BYTES <= QA_TILE_BYTES, "eight bf16 rows fit a stage");
+static_assert(QA_ROWS16 * ROW_BYTES <= QA_V_OFF, "eight bf16 rows fit a stage");
 constexpr float QA_SLACK = 8.f;                              // by how much (log2) a logit may pass the softmax reference
+constexpr int QA_PLAN = 128;                                 // tiles looked up ahead of the copies
+constexpr int QA_NEW = 1, QA_FLUSH = 2, QA_END = 4;          // first, last tile of a sequence for this warp; nothing comes after it
 
 struct Q4AttnArgs {
   LayerView v;
   Q4Pages p;
-  FastDiv by_g, by_tiles4, by_tiles16;      // by G; by the tiles of a chunk of either kind
-  int dense, T, G, causal, splits;
+  FastDiv by_g, by_h, by_k;                 // by G, by KV heads, by k
+  FastDiv by_tiles4, by_tiles16;            // by the tiles of a chunk of either kind
+  int dense, T, G, causal, k, groups;
   const uint16_t* q;
   uint16_t* out;
   float* lse;
   float scale;
-  float* partials;      // [S][splits][T G][132]
-  int32_t* counters;    // [row groups][S]
+  float* partials;      // the record of (sequence s, group, run c) at (s + c) groups + group: [query rows of a CTA][132]
+  int32_t* counters;    // [S][groups], zero between launches
 };
 
 template <int NT> struct QaShape {
   static constexpr int COLS = 8 * NT;                        // query rows of a CTA
-  static constexpr int STAGES = NT == 1 ? 3 : 5;
-  static constexpr int CTAS = NT == 1 ? 2 : 1;               // per SM
-  static constexpr int RING = QA_WARPS * STAGES * QA_TILE_BYTES;
-  static constexpr int MERGE = QA_WARPS * COLS * ATTN_PARTIAL_FLOATS * 4;      // the warps' states, in place of the ring
-  static constexpr int OFF_Q = RING > MERGE ? RING : MERGE;  // query rows, bf16
-  static constexpr int OFF_BAR = OFF_Q + COLS * ROW_BYTES;
-  static constexpr int SMEM = OFF_BAR + QA_WARPS * STAGES * 8 + 16;
+  static constexpr int CW = NT == 1 ? 12 : 8;                // consumer warps
+  static constexpr int PRODUCERS = 2, PLANNER = CW + PRODUCERS, MERGER = PLANNER + 1, WARPS = MERGER + 1;
+  static constexpr int STAGES = 3;                           // per consumer
+  static constexpr int OFF_STATE = CW * STAGES * QA_TILE_BYTES;                          // [consumers][query rows][132]: behind the ring
+  static constexpr int OFF_Q = OFF_STATE + CW * COLS * ATTN_PARTIAL_FLOATS * 4;          // [2][query rows][128] bf16; the same as fp16; what undoes their powers of two: [2][query rows]
+  static constexpr int OFF_QH = OFF_Q + 2 * COLS * ROW_BYTES;
+  static constexpr int OFF_UNDO = OFF_QH + 2 * COLS * ROW_BYTES;
+  static constexpr int OFF_INFO = OFF_UNDO + 2 * COLS * 4;   // [consumers][stages] int4: the tile's entry of the table
+  static constexpr int OFF_PLAN = OFF_INFO + CW * STAGES * 16;      // [QA_PLAN] int4: tiles looked up
+  static constexpr int OFF_BAR = OFF_PLAN + QA_PLAN * 16;
+  static constexpr int SMEM = OFF_BAR + (2 * CW * STAGES + 3) * 8 + 16 + (CW + 2) * 4;
+  static_assert(OFF_INFO % 16 == 0 && OFF_BAR % 8 == 0 && SMEM <= 227 * 1024, "shared memory of an SM");
 };
 
-// a tile as one lane knows it: where its rows lie (byte offset in the 4-bit pool, or element offset in the bf16 pool), how many, of which kind
-struct QaTile { long long at; int rows, kind; };
-
-__device__ __forceinline__ void mma_bf16_1688(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t b0) {
-  asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5}, {%6}, {%0,%1,%2,%3};"
-               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(b0));
+__device__ __forceinline__ int load_now(const int32_t* p) { return *reinterpret_cast<const volatile int32_t*>(p); }
+__device__ __forceinline__ float2 f16_pair(uint32_t w) {
+  float2 d;
+  asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.f32.f16 %0, a;\n\tcvt.f32.f16 %1, b;\n\t}" : "=f"(d.x), "=f"(d.y) : "r"(w));
+  return d;
 }
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+  uint32_t d;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+  return d;
+}
+// MMAs that start from zero, or go on with a sum (not volatile, unlike the one in common.cuh: the compiler may move them past one another)
+#define QA_MMA(NAME, TYPES)                                                                                                                        \
+  __device__ __forceinline__ void NAME##_first(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {                                \
+    asm("mma.sync.aligned.m16n8k16.row.col.f32." TYPES ".f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"                             \
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));               \
+  }                                                                                                                                              \
+  __device__ __forceinline__ void NAME##_next(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {                                 \
+    asm("mma.sync.aligned.m16n8k16.row.col.f32." TYPES ".f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"                                 \
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));                         \
+  }
+QA_MMA(mma_f16, "f16.f16")
+QA_MMA(mma_bf16, "bf16.bf16")
+#undef QA_MMA
 __device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
   uint32_t d;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(x));
-  return d;
-}
-__device__ __forceinline__ uint32_t sub_bf16x2(uint32_t a, uint32_t b) {
-  uint32_t d;
-  asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(x));
   return d;
 }
 
-// NT: column tiles of eight query rows; SPLIT (NT == 1): up to four query rows, their weights' two planes side by side in the columns
-template <int NT, bool SPLIT>
-__global__ void __launch_bounds__(QA_WARPS * 32, QaShape<NT>::CTAS) kve_decode_attn_q4_kernel(Q4AttnArgs a) {
+// word i of four (i known at compile time)
+__device__ __forceinline__ uint32_t word_of(const uint4& w, int i) { return i == 0 ? w.x : (i == 1 ? w.y : (i == 2 ? w.z : w.w)); }
+// folds a state (accumulator, reference, sum) into one with reference `top`
+__device__ __forceinline__ void fold(const float* st, float top, float& sum, float4& o, int lane) {
+  const float m = st[128], f = m == -INFINITY ? 0.f : exp2f(m - top);
+  const float4 x = *reinterpret_cast<const float4*>(st + lane * 4);
+  sum = fmaf(st[129], f, sum);
+  o.x = fmaf(x.x, f, o.x); o.y = fmaf(x.y, f, o.y); o.z = fmaf(x.z, f, o.z); o.w = fmaf(x.w, f, o.w);
+}
+// a warp writes query row rr of sequence s
+__device__ __forceinline__ void write_row(const Q4AttnArgs& a, int s, int rr, float4 o, float top, float sum, int lane) {
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;      // (no row, or weights of 0 only: 0; NaN stays)
+  const int t = (int)a.by_g.div((uint32_t)rr), g = rr - t * a.G, b = (int)a.by_h.div((uint32_t)s), h = s - b * a.v.H;
+  const long long at = (((long long)b * a.T + t) * a.v.H + h) * a.G + g;
+  *reinterpret_cast<uint2*>(a.out + at * D + lane * 4) = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
+  if (a.lse && lane == 0) a.lse[at] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.69314718055994530942f;
+}
+
+// CTA c of P takes parts [c I / P, (c + 1) I / P) (32-bit arithmetic: the host keeps I P below 2^32)
+__device__ __forceinline__ uint32_t qa_begin(uint32_t c, uint32_t I, uint32_t P) { return (c * I) / P; }
+__device__ __forceinline__ uint32_t qa_owner(uint32_t x, uint32_t I, uint32_t P) { return ((x + 1u) * P - 1u) / I; }
+
+// NT: column tiles of eight query rows
+template <int NT>
+__global__ void __launch_bounds__(QaShape<NT>::WARPS * 32, 1) kve_decode_attn_q4_kernel(Q4AttnArgs a) {
   using Shape = QaShape<NT>;
-  constexpr int STAGES = Shape::STAGES;
-  constexpr int PER_GROUP = SPLIT ? 4 : Shape::COLS;      // query rows of this CTA
+  constexpr int STAGES = Shape::STAGES, CW = Shape::CW, WARPS = Shape::WARPS, COLS = Shape::COLS;
   extern __shared__ __align__(128) unsigned char smem[];
-  uint16_t* Qs = reinterpret_cast<uint16_t*>(smem + Shape::OFF_Q);
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + Shape::OFF_BAR);
-  int* flag = reinterpret_cast<int*>(bars + QA_WARPS * STAGES);
   const LayerView& v = a.v;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g8 = lane >> 2, t4 = lane & 3;
-  const int part = blockIdx.x, s = blockIdx.y, z = blockIdx.z;
-  const int R = a.T * a.G, row0 = z * PER_GROUP, n_rows = min(R - row0, PER_GROUP);
-  uint64_t* full = bars + warp * STAGES;
-  unsigned char* ring = smem + warp * STAGES * QA_TILE_BYTES;
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + Shape::OFF_BAR);      // [consumers][stages]
+  uint64_t* empty = full + CW * STAGES;
+  uint64_t* left = empty + CW * STAGES;      // all consumers have left their state of a sequence
+  uint64_t* merged = left + 1;               // which has been folded, and the query rows of the sequence after the next brought
+  uint64_t* fetched = merged + 1;            // the query rows of the first two sequences are there
+  int* flags = reinterpret_cast<int*>(fetched + 1);      // at the end: records of the first and of the last sequence, where this CTA merges them
+  volatile int* progress = flags + 4;                    // [consumers] the entry of the table that each will need next; behind them: entries there are; tokens stored
+  int4* plan = reinterpret_cast<int4*>(smem + Shape::OFF_PLAN);
+  int4* infos = reinterpret_cast<int4*>(smem + Shape::OFF_INFO);
+  float* states = reinterpret_cast<float*>(smem + Shape::OFF_STATE);
+  const int R = a.T * a.G;
+  const float sl2 = a.scale * 1.44269504088896340736f;      // logits in log2 units
 
   pdl_launch_dependents();
-  if (lane < STAGES) mbar_init(&full[lane], 1);
+  for (int i = threadIdx.x; i < 2 * CW * STAGES; i += WARPS * 32) mbar_init(&full[i], 1);
+  if (threadIdx.x == 0) {
+    mbar_init(left, CW);
+    mbar_init(merged, 1);
+    mbar_init(fetched, 1);
+    progress[CW] = 0;
+  }
+  if (threadIdx.x < CW) progress[threadIdx.x] = threadIdx.x;
   mbar_fence_init();
-  __syncwarp();
+  // the run of this CTA: parts i0 .. i1 - 1 of the sequences x0 .. x1, for one group of query rows
+  const uint32_t uk = (uint32_t)a.k, n_items = (uint32_t)v.S * uk, P = gridDim.x / (uint32_t)a.groups;
+  const int run = (int)(blockIdx.x / (uint32_t)a.groups), group = (int)blockIdx.x - run * a.groups;
+  const int row0 = group * COLS, n_rows = min(R - row0, COLS);      // its query rows
+  const uint32_t i0 = qa_begin((uint32_t)run, n_items, P), i1 = qa_begin((uint32_t)run + 1u, n_items, P);
+  const int x0 = (int)a.by_k.div(i0), x1 = (int)a.by_k.div(i1 - 1u);      // (i0 < i1: there are no more runs than parts)
+  __syncthreads();
   pdl_wait();
 
-  // ---- the lists: kept chunks in 4 bits, chunks behind the keep list in 4 bits, kept chunks in bf16, the rest in bf16 ----
-  const int n = min(max(*reinterpret_cast<const volatile int32_t*>(v.seq_len), 0), v.max_tokens);
-  const int packed = min(max(*reinterpret_cast<const volatile int32_t*>(v.n_packed), 0), n / v.C);
-  const int listed = a.dense ? 0 : min(max(*reinterpret_cast<const volatile int32_t*>(v.n_listed), 0), n / v.C);
-  const long long sb = (long long)s * v.max_chunks;
-  const int kept = a.dense ? 0 : min(max(*reinterpret_cast<const volatile int32_t*>(v.keep_cnt + s), 0), listed);
-  int kept4 = kept;      // kept chunks that are packed: the list ascends
-  if (packed < listed) {
-    int lo = 0, hi = kept;
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (__ldcg(v.keep_idx + sb + mid) < packed) lo = mid + 1; else hi = mid;
-    }
-    kept4 = lo;
-  }
-  const int c_tail = max(listed, packed), tail = n - c_tail * v.C;
-  const int per4 = (v.C + QA_ROWS4 - 1) / QA_ROWS4, per16 = v.C / QA_ROWS16;
-  const int e0 = kept4 * per4, e1 = e0 + max(packed - listed, 0) * per4, e2 = e1 + (kept - kept4) * per16, total = e2 + (tail + QA_ROWS16 - 1) / QA_ROWS16;
-  const int j0 = (int)((long long)part * total / a.splits), j1 = (int)((long long)(part + 1) * total / a.splits);
-  const int mine = max(0, (j1 - j0 - warp + QA_WARPS - 1) / QA_WARPS);      // tiles of this warp: j0 + warp, + 8, ...
-  if (a.causal && tail < a.T && threadIdx.x == 0) set_status(v.status, ERR_CAPACITY);      // (a replay that outgrew its capture: the block's first tokens have no rows of their own any more)
-
-  // Where the tile this lane looks after lies.  In two steps, so that no look-up is waited for: the chunk, then its page.
-  auto chunk_of = [&](int i) -> int {      // i: index among this warp's tiles; -1: none
-    if (i >= mine) return -1;
-    const int j = j0 + warp + i * QA_WARPS;
-    if (j < e0) return __ldcg(v.keep_idx + sb + (int)a.by_tiles4.div((uint32_t)j));
-    if (j < e1) return listed + (int)a.by_tiles4.div((uint32_t)(j - e0));
-    if (j < e2) return __ldcg(v.keep_idx + sb + kept4 + (int)a.by_tiles16.div((uint32_t)(j - e1)));
-    return c_tail + (int)a.by_tiles16.div((uint32_t)(j - e2));
-  };
-  auto page_of = [&](int i, int chunk) -> int {
-    if (i >= mine || chunk < 0 || chunk >= v.max_chunks) return -1;
-    return __ldcg((j0 + warp + i * QA_WARPS < e1 ? a.p.table : v.page_table) + sb + chunk);
-  };
-  auto tile_of = [&](int i, int page) -> QaTile {
-    QaTile t;
-    t.at = 0; t.rows = 0; t.kind = 0;
-    if (i >= mine) return t;
-    const int j = j0 + warp + i * QA_WARPS;
-    t.kind = j < e1 ? 0 : 1;
-    if (t.kind == 0) {
-      const int jj = j < e0 ? j : j - e0, within = jj - (int)a.by_tiles4.div((uint32_t)jj) * per4;
-      t.rows = min(QA_ROWS4, v.C - within * QA_ROWS4);
-      if (page < 0 || page >= a.p.n_pages) { set_status(v.status, ERR_CAPACITY); page = 0; }
-      t.at = ((long long)page * v.C + within * QA_ROWS4) * (Q4_UNIT_BYTES / Q4_UNIT_ROWS);
-    } else {
-      const int jj = j < e2 ? j - e1 : j - e2, within = jj - (int)a.by_tiles16.div((uint32_t)jj) * per16;
-      t.rows = j < e2 ? QA_ROWS16 : min(QA_ROWS16, tail - jj * QA_ROWS16);
-      if (page < 0 || page >= v.n_pages) { set_status(v.status, ERR_CAPACITY); page = 0; }
-      t.at = ((long long)page * v.C + within * QA_ROWS16) * D;
-    }
-    return t;
-  };
-  const int chunk0 = chunk_of(lane);
-  QaTile cur = tile_of(lane, page_of(lane, chunk0));
-  int next_chunk = -1, next_page = -1;      // of the tile 32 on
-  // asks for tile i; i runs through 0, 1, 2, ...
-  auto issue = [&](int i) {
-    const int l = i & 31, stage = i % STAGES;
-    if (l == 0 && i > 0) cur = tile_of(i + lane, next_page);
-    if (l == 8) next_chunk = chunk_of((i & ~31) + 32 + lane);
-    if (l == 20) next_page = page_of((i & ~31) + 32 + lane, next_chunk);
-    unsigned char* dst = ring + stage * QA_TILE_BYTES;
-    const int kind = __shfl_sync(0xffffffffu, cur.kind, l), rows = __shfl_sync(0xffffffffu, cur.rows, l);
-    const long long at = __shfl_sync(0xffffffffu, cur.at, l);
-    if (kind == 0) {
-      if (lane == 0) {
-        const uint32_t bytes = (uint32_t)rows * (Q4_UNIT_BYTES / Q4_UNIT_ROWS);
-        mbar_arrive_expect_tx(&full[stage], 2 * bytes);
-        bulk_g2s(dst, a.p.k + at, bytes, &full[stage]);
-        bulk_g2s(dst + QA_V_OFF, a.p.v + at, bytes, &full[stage]);
+  // ---- a warp brings the query rows of sequence s into slot `slot`: bf16, and fp16 times a power of two ----
+  auto fetch_queries = [&](int s, int slot) {
+    uint32_t* Qh = reinterpret_cast<uint32_t*>(smem + Shape::OFF_QH) + slot * COLS * 64;
+    uint4* Qb = reinterpret_cast<uint4*>(smem + Shape::OFF_Q) + slot * COLS * 16;
+    float* q_undo = reinterpret_cast<float*>(smem + Shape::OFF_UNDO) + slot * COLS;
+    const int b = (int)a.by_h.div((uint32_t)s), h = s - b * v.H, piece = lane & 15;
+#pragma unroll 4
+    for (int c = lane >> 4; c < COLS; c += 2) {      // column c of the MMAs is query row row0 + c; rows that do not exist are zeros.  Half a warp a row
+      uint4 w = make_uint4(0u, 0u, 0u, 0u);
+      if (c < n_rows) {
+        const int t = (int)a.by_g.div((uint32_t)(row0 + c)), gq = row0 + c - t * a.G;
+        w = __ldcg(reinterpret_cast<const uint4*>(a.q + ((((long long)b * a.T + t) * v.H + h) * a.G + gq) * D + piece * 8));
       }
+      Qb[c * 16 + piece] = w;
+      const uint32_t word[4] = {w.x, w.y, w.z, w.w};
+      float most = 0.f;      // of the finite ones
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float p = fabsf(bf16lo(word[e])), q = fabsf(bf16hi(word[e]));
+        most = fmaxf(most, fmaxf(p < INFINITY ? p : 0.f, q < INFINITY ? q : 0.f));
+      }
+#pragma unroll
+      for (int o = 1; o <= 8; o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+      const int power = most > 0.f ? min(max(14 - ((int)(__float_as_uint(most) >> 23) - 127), -100), 120) : 0;
+      const float up = __uint_as_float((uint32_t)(127 + power) << 23);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {      // odd pairs meet codes that are 2^4 times as large
+        const float f = e & 1 ? up * 0.0625f : up;
+        Qh[c * 64 + piece * 4 + e] = pack_f16x2(bf16lo(word[e]) * f, bf16hi(word[e]) * f);
+      }
+      if (piece == 0) q_undo[c] = __uint_as_float((uint32_t)(127 - power) << 23);
+    }
+  };
+  // folds the consumers' states of query row r of sequence x: the result, or a record
+  auto fold_states = [&](int x, int r) {
+    const float* st = states + r * ATTN_PARTIAL_FLOATS;
+    float top = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < CW; ++w) top = fmaxf(top, st[w * COLS * ATTN_PARTIAL_FLOATS + 128]);
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < CW; ++w) fold(st + w * COLS * ATTN_PARTIAL_FLOATS, top, sum, o, lane);
+    if (qa_owner((uint32_t)x * uk, n_items, P) == qa_owner((uint32_t)(x + 1) * uk - 1u, n_items, P)) {
+      write_row(a, x, row0 + r, o, top, sum, lane);
     } else {
-      if (lane == 0) mbar_arrive_expect_tx(&full[stage], (uint32_t)rows * 2 * ROW_BYTES);
+      float* rec = a.partials + (((long long)(x + run) * a.groups + group) * COLS + r) * ATTN_PARTIAL_FLOATS;
+      *reinterpret_cast<float4*>(rec + lane * 4) = o;
+      if (lane == 0) { rec[128] = top; rec[129] = sum; }
+    }
+  };
+
+  if (warp == Shape::PLANNER) {
+    // ================= planner: looks up tiles, 32 side by side =================
+    const int len = load_now(v.seq_len), dev_packed = load_now(v.n_packed), dev_listed = a.dense ? 0 : load_now(v.n_listed);
+    int dev_kept = a.dense ? 0 : load_now(v.keep_cnt + x0);      // (all four on their way together)
+    const int n = min(max(len, 0), v.max_tokens), complete = n / v.C;
+    const int packed = min(max(dev_packed, 0), complete), listed = min(max(dev_listed, 0), complete);
+    if (lane == 0) progress[CW + 1] = n;
+    const int per4 = (v.C + QA_ROWS4 - 1) / QA_ROWS4, per16 = v.C / QA_ROWS16;
+    const int c_tail = max(listed, packed), tail = n - c_tail * v.C;      // the rest in bf16: first chunk, rows
+    if (a.causal && tail < a.T && lane == 0) set_status(v.status, ERR_CAPACITY);      // (a replay that outgrew its capture: the block's first tokens have no rows of their own any more)
+    // The table's entries are numbered through; entry i is consumer i % CW's.  A sequence has at least CW of them, so that every consumer learns of it.
+    int x = x0, j = 0, j_end = 0, pos_in = 0, n_entries = 0;      // sequence being looked up; its next tile and last; entries it has so far, and will have
+    int e0 = 0, e1 = 0, e2 = 0, kept4 = 0;                        // in tiles: kept chunks in 4 bits up to e0; chunks behind the keep list in 4 bits up to e1; kept chunks in bf16 up to e2; the rest in bf16
+    int planned = 0;
+    auto enter = [&]() {
+      const long long sb = (long long)x * v.max_chunks;
+      const int kept = min(max(dev_kept, 0), listed);
+      if (!a.dense && x < x1) dev_kept = load_now(v.keep_cnt + x + 1);      // the next one's
+      kept4 = kept;      // kept chunks that are packed: the list ascends
+      if (packed < listed) {
+        int lo = 0, hi = kept;
+        while (lo < hi) {
+          const int mid = (lo + hi) >> 1;
+          if (__ldcg(v.keep_idx + sb + mid) < packed) lo = mid + 1; else hi = mid;
+        }
+        kept4 = lo;
+      }
+      e0 = kept4 * per4;
+      e1 = e0 + max(packed - listed, 0) * per4;
+      e2 = e1 + (kept - kept4) * per16;
+      const int total = e2 + (tail + QA_ROWS16 - 1) / QA_ROWS16;
+      const uint32_t p_lo = x == x0 ? i0 - (uint32_t)x * uk : 0u, p_hi = x == x1 ? i1 - (uint32_t)x * uk : uk;
+      j = (int)((long long)p_lo * total / a.k);
+      j_end = (int)((long long)p_hi * total / a.k);
+      pos_in = 0;
+      n_entries = max(j_end - j, CW);
+    };
+    // the next entries, up to 32 of one sequence, a lane each
+    auto look_up = [&]() {
+      const int jj = j + lane, at = pos_in + lane, count = min(32, n_entries - pos_in);
+      int4 e = make_int4(0, 0, 0, 0);      // page, first row in it, rows (negative: bf16 ones; 0: none), flags and the position of the first row
+      if (jj < j_end) {
+        const long long sb = (long long)x * v.max_chunks;
+        const int of = jj < e0 ? jj : (jj < e1 ? jj - e0 : (jj < e2 ? jj - e1 : jj - e2));      // in its list
+        const bool in4 = jj < e1;
+        const int nth = (int)(in4 ? a.by_tiles4 : a.by_tiles16).div((uint32_t)of), within = of - nth * (in4 ? per4 : per16);
+        int chunk;
+        if (jj < e0) chunk = __ldcg(v.keep_idx + sb + nth);
+        else if (jj < e1) chunk = listed + nth;
+        else if (jj < e2) chunk = __ldcg(v.keep_idx + sb + kept4 + nth);
+        else chunk = c_tail + nth;
+        int page = chunk >= 0 && chunk < v.max_chunks ? __ldcg((in4 ? a.p.table : v.page_table) + sb + chunk) : -1;
+        if (page < 0 || page >= (in4 ? a.p.n_pages : (long long)v.n_pages)) { set_status(v.status, ERR_CAPACITY); page = 0; }
+        e.x = page;
+        e.y = within * (in4 ? QA_ROWS4 : QA_ROWS16);
+        e.z = in4 ? min(QA_ROWS4, v.C - e.y) : -(jj < e2 ? QA_ROWS16 : min(QA_ROWS16, tail - of * QA_ROWS16));
+        e.w = (chunk * v.C + e.y) << 3;
+      }
+      const bool last = at + CW >= n_entries;
+      e.w |= (at < CW ? QA_NEW : 0) | (last ? QA_FLUSH : 0) | (last && x == x1 ? QA_END : 0);
+      if (lane < count) plan[(planned + lane) % QA_PLAN] = e;
+      planned += count;
+      pos_in += count;
+      j += count;
+      if (pos_in == n_entries && ++x <= x1) enter();
       __syncwarp();
-      const int r = lane & 7;
-      if (lane < 16 && r < rows) {
-        if (lane < 8) bulk_g2s(dst + qa_k_row(r), v.k_pages + at + r * D, ROW_BYTES, &full[stage]);
-        else bulk_g2s(dst + qa_v_row(r), v.v_pages + at + r * D, ROW_BYTES, &full[stage]);
+    };
+    enter();
+    for (int idle = 0; x <= x1;) {
+      // room for 32 more: entries that all have come past
+      if (planned + 32 - (int)__reduce_min_sync(0xffffffffu, lane < CW ? (unsigned)progress[lane] : 0xffffffffu) <= QA_PLAN) {
+        look_up();
+        __threadfence_block();
+        __syncwarp();
+        if (lane == 0) progress[CW] = planned;
+        idle = 0;
+      } else {
+        __nanosleep(200);
+        if (++idle > (1 << 20)) {
+          if (lane == 0) set_status(v.status, ERR_TIMEOUT);
+          break;
+        }
       }
     }
-  };
-  for (int i = 0; i < STAGES && i < mine; ++i) issue(i);
-
-  // ---- query rows: operand fragments, and the sums of their two halves ----
-  // column c of the MMAs is query row row0 + (SPLIT ? c & 3 : c); rows that do not exist are zeros
-  for (int i = threadIdx.x; i < Shape::COLS * 16; i += QA_WARPS * 32) {
-    const int c = i >> 4, r = SPLIT ? (c & 3) : c;
-    uint4 w = make_uint4(0u, 0u, 0u, 0u);
-    if (r < n_rows) {
-      const int rr = row0 + r, t = (int)a.by_g.div((uint32_t)rr), g = rr - t * a.G;
-      const int b = s / v.H, h = s - b * v.H;
-      w = __ldcg(reinterpret_cast<const uint4*>(a.q + ((((long long)b * a.T + t) * v.H + h) * a.G + g) * D + (i & 15) * 8));
-    }
-    *reinterpret_cast<uint4*>(Qs + c * D + (i & 15) * 8) = w;
-  }
-  __syncthreads();
-  constexpr bool Q_REGS = NT == 1;
-  uint4 qf[Q_REGS ? 4 : 1];      // column g8: the numbers 32 j + 8 t4 .. + 7
-  if constexpr (Q_REGS) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) qf[j] = *reinterpret_cast<const uint4*>(Qs + g8 * D + 32 * j + 8 * t4);
-  }
-  float qsum[NT][2][2];          // [half][column 2 t4, 2 t4 + 1]
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      float sum = 0.f;
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const uint4 w = *reinterpret_cast<const uint4*>(Qs + (nt * 8 + g8) * D + 64 * h + 32 * j + 8 * t4);
-        sum += (bf16lo(w.x) + bf16hi(w.x)) + (bf16lo(w.y) + bf16hi(w.y)) + (bf16lo(w.z) + bf16hi(w.z)) + (bf16lo(w.w) + bf16hi(w.w));
+  } else if (warp >= CW && warp < Shape::PLANNER) {
+    // ================= producers: a lane fills the ring of a consumer =================
+    const int w = (warp - CW) * (CW / Shape::PRODUCERS) + lane;      // that consumer
+    uint64_t *my_full = full + w * STAGES, *my_empty = empty + w * STAGES;
+    int pushed = 0, entry = w, idle = 0;      // tiles asked for; the next one's entry
+    const bool mine = lane < CW / Shape::PRODUCERS;
+    bool active = mine;
+    while (__any_sync(0xffffffffu, active)) {
+      const int stage = pushed % STAGES, round = pushed / STAGES;
+      const bool ready = active && entry < progress[CW] && (round == 0 || mbar_test_wait(&my_empty[stage], (uint32_t)(round - 1) & 1u));
+      if (ready) {
+        __threadfence_block();
+        const int4 e = plan[entry % QA_PLAN];
+        infos[w * STAGES + stage] = e;
+        if (e.z != 0) {
+          unsigned char* dst = smem + (w * STAGES + stage) * QA_TILE_BYTES;
+          const bool in4 = e.z > 0;
+          const uint32_t row_bytes = in4 ? Q4_UNIT_BYTES / Q4_UNIT_ROWS : ROW_BYTES, bytes = (uint32_t)abs(e.z) * row_bytes;
+          const long long at = ((long long)e.x * v.C + e.y) * row_bytes;
+          mbar_arrive_expect_tx(&my_full[stage], 2 * bytes);      // release: whoever sees the phase sees the description
+          bulk_g2s(dst, (in4 ? a.p.k : reinterpret_cast<const uint8_t*>(v.k_pages)) + at, bytes, &my_full[stage]);
+          bulk_g2s(dst + QA_V_OFF, (in4 ? a.p.v : reinterpret_cast<const uint8_t*>(v.v_pages)) + at, bytes, &my_full[stage]);
+        } else {
+          mbar_arrive(&my_full[stage]);
+        }
+        ++pushed;
+        entry += CW;
+        __threadfence_block();
+        progress[w] = active && (e.w & QA_END) ? 0x7fffffff : entry;      // (the planner may write over what this lane has read)
+        active = (e.w & QA_END) == 0;
       }
-      sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-      sum += __shfl_xor_sync(0xffffffffu, sum, 2);      // of column g8, in its four lanes
-      qsum[nt][h][0] = __shfl_sync(0xffffffffu, sum, 8 * t4);
-      qsum[nt][h][1] = __shfl_sync(0xffffffffu, sum, 8 * t4 + 4);
+      if (__any_sync(0xffffffffu, ready)) {
+        idle = 0;
+      } else {
+        __nanosleep(100);
+        if (++idle > (1 << 20)) {
+          if (lane == 0) set_status(v.status, ERR_TIMEOUT);
+          break;
+        }
+      }
     }
-  const float sl2 = a.scale * 1.44269504088896340736f;      // logits in log2 units
-  int last_pos[NT][2];                                       // causal: the last position a column sees
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const int c = nt * 8 + 2 * t4 + x, rr = row0 + (SPLIT ? (c & 3) : c);
-      last_pos[nt][x] = a.causal ? n - a.T + (int)a.by_g.div((uint32_t)min(rr, R - 1)) : 0x7fffffff;
+    // nobody leaves with copies under way: their consumers see all of them land, unless one has given up
+    if (mine) ring_drain<STAGES>(my_full, pushed);
+  } else if (warp == Shape::MERGER) {
+    // ================= merger: brings query rows, folds the states of all sequences but the last =================
+    fetch_queries(x0, 0);
+    if (x1 > x0) fetch_queries(x0 + 1, 1);
+    __syncwarp();
+    if (lane == 0) mbar_arrive(fetched);
+    for (int x = x0; x < x1; ++x) {
+      if (!mbar_wait_bounded(left, (uint32_t)(x - x0) & 1u)) {
+        if (lane == 0) set_status(v.status, ERR_TIMEOUT);
+        break;
+      }
+      for (int r = 0; r < n_rows; ++r) fold_states(x, r);
+      __syncwarp();
+      if (x + 2 <= x1) fetch_queries(x + 2, (x - x0) & 1);
+      __threadfence_block();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(merged);
     }
+  } else {
+    // ================= consumers =================
+    // ---- the sequence under way ----
+    const uint16_t *Qh = nullptr, *Qb = nullptr;      // its query rows, as fp16 and as bf16
+    // column nt 8 + g8: the numbers 32 j + 8 t4 .. + 7, as fp16 (from shared memory every time)
+    auto q_half = [&](int nt, int j) { return *reinterpret_cast<const uint4*>(Qh + (nt * 8 + g8) * D + 32 * j + 8 * t4); };
+    float undo[NT][2], qsum[NT][2][2];      // per column 2 t4, 2 t4 + 1: what takes q's power of two off a sum of codes (2^-24) and makes it a log2 logit; sums of q over the halves
+    int n = 0;                              // tokens stored (read where it matters)
+    auto last_pos = [&](int nt, int x) {    // causal: the last position a column sees
+      return a.causal ? n - a.T + (int)a.by_g.div((uint32_t)min(row0 + nt * 8 + 2 * t4 + x, R - 1)) : 0x7fffffff;
+    };
 
-  float acc[NT][8][4];           // [m]: dims d = 64 (m / 4) + 8 g8 + 2 (m % 4) and d + 1, columns 2 t4 and 2 t4 + 1: (d, c), (d, c + 1), (d + 1, c), (d + 1, c + 1)
-  float ref[NT][2], l[NT][2], zs[NT][2][2];      // per column: reference; this lane's rows' share of the sum of weights, and of weights times what the codes' offset stands for
+    float acc[NT][8][4];           // [m]: dims d = 64 (m / 4) + 8 g8 + 2 (m % 4) and d + 1, columns 2 t4 and 2 t4 + 1: (d, c), (d, c + 1), times F 2^-24; (d + 1, c), (d + 1, c + 1), times F 2^-20
+    float l[NT][2], zs[NT][2][2];  // this lane's rows' share, per column: sum of weights; of weights times what code 0 stands for
+    // per column: the softmax's reference (0 until there is one), and what a logit may exceed it by (-inf until there is one)
+    float ref[NT][2], over_by[NT][2];
+    float F[2];      // weight factor of either half: the largest p s so far times F lies in [2^6, 2^7); a scale with s F > 2^7 asks for another
+    // a fresh state, and the query rows in slot `slot`
+    auto start = [&](int slot) {
+      Qh = reinterpret_cast<const uint16_t*>(smem + Shape::OFF_QH) + slot * COLS * D;
+      Qb = reinterpret_cast<const uint16_t*>(smem + Shape::OFF_Q) + slot * COLS * D;
+      const float* q_undo = reinterpret_cast<const float*>(smem + Shape::OFF_UNDO) + slot * COLS;
+      F[0] = F[1] = 0x1p120f;
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
+      for (int nt = 0; nt < NT; ++nt) {
+        float sum[2] = {0.f, 0.f};
 #pragma unroll
-    for (int m = 0; m < 8; ++m)
+        for (int j = 0; j < 4; ++j) {
+          const uint4 w = q_half(nt, j);
+          const float2 e0 = f16_pair(w.x), e1 = f16_pair(w.y), e2 = f16_pair(w.z), e3 = f16_pair(w.w);
+          sum[j >> 1] += (e0.x + e0.y) + (e2.x + e2.y) + 16.f * ((e1.x + e1.y) + (e3.x + e3.y));
+        }
+        const float off = q_undo[nt * 8 + g8] * sl2;
 #pragma unroll
-      for (int x = 0; x < 4; ++x) acc[nt][m][x] = 0.f;
+        for (int h = 0; h < 2; ++h) {
+          float y = sum[h];
+          y += __shfl_xor_sync(0xffffffffu, y, 1);
+          y += __shfl_xor_sync(0xffffffffu, y, 2);      // of column g8, in its four lanes
+          y *= off;
+          qsum[nt][h][0] = __shfl_sync(0xffffffffu, y, 8 * t4);
+          qsum[nt][h][1] = __shfl_sync(0xffffffffu, y, 8 * t4 + 4);
+        }
 #pragma unroll
-    for (int x = 0; x < 2; ++x) { ref[nt][x] = -INFINITY; l[nt][x] = 0.f; zs[nt][0][x] = zs[nt][1][x] = 0.f; }
-  }
+        for (int c = 0; c < 2; ++c) {
+          undo[nt][c] = q_undo[nt * 8 + 2 * t4 + c] * 0x1p12f * sl2 * 0x1p12f;
+          ref[nt][c] = 0.f; over_by[nt][c] = -INFINITY; l[nt][c] = 0.f; zs[nt][0][c] = zs[nt][1][c] = 0.f;
+        }
+#pragma unroll
+        for (int m = 0; m < 8; ++m)
+#pragma unroll
+          for (int y = 0; y < 4; ++y) acc[nt][m][y] = 0.f;
+      }
+    };
 
-  // Logits of 16 rows (log2 units; [row g8: c, c + 1; row g8 + 8: c, c + 1]) to weights in place; raises the reference where it has to
-  auto weigh = [&](float (&x)[NT][4]) {
-    bool over = false;
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) over |= x[nt][i] > ref[nt][i & 1] + QA_SLACK;
-    if (__any_sync(0xffffffffu, over)) {
+    // Logits minus reference (log2 units; of each of this lane's rows: c, c + 1) to weights in place.  s0, s1: the largest scale of
+    // these rows in either half.  Raises reference and factors where it has to.
+    auto weigh = [&](auto& x, float s0, float s1) {
+      constexpr int N = (int)(sizeof(x[0]) / sizeof(float));
+      bool over = s0 * F[0] > 128.f || s1 * F[1] > 128.f;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          float top = fmaxf(x[nt][c], x[nt][2 + c]);
+        for (int i = 0; i < N; ++i) over |= x[nt][i] > over_by[nt][i & 1];
+      if (__any_sync(0xffffffffu, over)) {
+        float most = 0.f;      // of the factors that the sums so far get
 #pragma unroll
-          for (int o = 4; o <= 16; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-          const float to = fmaxf(ref[nt][c], top);
-          const float f = to == -INFINITY ? 1.f : ex2_fast(ref[nt][c] - to);
-          ref[nt][c] = to;
-          l[nt][c] *= f; zs[nt][0][c] *= f; zs[nt][1][c] *= f;
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int m = 0; m < 8; ++m) { acc[nt][m][c] *= f; acc[nt][m][2 + c] *= f; }
-        }
-    }
+          for (int c = 0; c < 2; ++c) {
+            float top = x[nt][c];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+            for (int i = c + 2; i < N; i += 2) top = fmaxf(top, x[nt][i]);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float r = ref[nt][i & 1];
-        x[nt][i] = ex2_fast(x[nt][i] - (r == -INFINITY ? 0.f : r));      // (only logits of -inf so far: weights 0)
-        l[nt][i & 1] += x[nt][i];
-      }
-  };
-  // two weights as bf16: the plane of the SPLIT column, or both planes
-  auto planes = [&](float w0, float w1, uint32_t& hi, uint32_t& lo) {
-    hi = pack_bf16x2(w0, w1);
-    lo = pack_bf16x2(w0 - bf16lo(hi), w1 - bf16hi(hi));
-    if (SPLIT) hi = t4 >= 2 ? lo : hi;
-  };
-
-  for (int i = 0; i < mine; ++i) {
-    const int stage = i % STAGES;
-    if (!mbar_wait_bounded(&full[stage], (uint32_t)((i / STAGES) & 1))) {
-      if (lane == 0) set_status(v.status, ERR_TIMEOUT);
-      ring_drain<STAGES>(full, min(i + STAGES, mine));
-      break;
-    }
-    const unsigned char* base = ring + stage * QA_TILE_BYTES;
-    const int j = j0 + warp + i * QA_WARPS;
-    if (j < e1) {
-      // ================= packed rows =================
-      const int jj = j < e0 ? j : j - e0, within = jj - (int)a.by_tiles4.div((uint32_t)jj) * per4;
-      const int units = min(2, per16 / 2 - within * 2);
-      for (int u = 0; u < units; ++u) {
-        const unsigned char* kb = base + u * Q4_UNIT_BYTES;
-        const unsigned char* vb = kb + QA_V_OFF;
-        const uint4 ka = *reinterpret_cast<const uint4*>(kb + lane * 16), kc = *reinterpret_cast<const uint4*>(kb + 512 + lane * 16);
-        const uint2 ha = *reinterpret_cast<const uint2*>(kb + Q4_CODE_BYTES + g8 * 8), hc = *reinterpret_cast<const uint2*>(kb + Q4_CODE_BYTES + 64 + g8 * 8);
-        float x[NT][4];
-        {
-          const uint32_t wa[4] = {ka.x, ka.y, ka.z, ka.w}, wc[4] = {kc.x, kc.y, kc.z, kc.w};
-          float d[NT][2][4];
+            for (int o = 4; o <= 16; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            const bool first = over_by[nt][c] == -INFINITY;
+            const float to = ref[nt][c] + (first ? (top == -INFINITY ? 0.f : top) : fmaxf(top, 0.f)), up = to - ref[nt][c];
+            const float f = first ? 1.f : ex2_fast(-up);
+            most = fmaxf(most, f);
+            if (top != -INFINITY) over_by[nt][c] = QA_SLACK;
+            ref[nt][c] = to;
+#pragma unroll
+            for (int i = c; i < N; i += 2) x[nt][i] -= up;
+            l[nt][c] *= f; zs[nt][0][c] *= f; zs[nt][1][c] *= f;
+#pragma unroll
+            for (int m = 0; m < 8; ++m) { acc[nt][m][c] *= f; acc[nt][m][2 + c] *= f; }
+          }
+        most = warp_max(most);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float largest = fmaxf(64.f / F[h] * most, warp_max(h ? s1 : s0));
+          const int e = min(max((int)(__float_as_uint(largest) >> 23) - 127, -110), 126);
+          const float to = __uint_as_float((uint32_t)(127 + 6 - e) << 23), f = to / F[h];
+          F[h] = to;
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int m = 0; m < 4; ++m)
 #pragma unroll
-              for (int y = 0; y < 4; ++y) d[nt][h][y] = 0.f;
+              for (int y = 0; y < 4; ++y) acc[nt][4 * h + m][y] *= f;
+        }
+      }
 #pragma unroll
-          for (int jw = 0; jw < 4; ++jw) {
-            uint32_t pa[4], pc[4];
-            q4_spread(wa[jw], pa);
-            q4_spread(wc[jw], pc);
-            const uint32_t A0[4] = {pa[0], pc[0], pa[1], pc[1]}, A1[4] = {pa[2], pc[2], pa[3], pc[3]};
+      for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              const uint4 qw = Q_REGS ? qf[Q_REGS ? jw : 0] : *reinterpret_cast<const uint4*>(Qs + (nt * 8 + g8) * D + 32 * jw + 8 * t4);
-              mma_bf16_16816(d[nt][jw >> 1], A0, qw.x, qw.y);
-              mma_bf16_16816(d[nt][jw >> 1], A1, qw.z, qw.w);
+        for (int i = 0; i < N; ++i) {
+          x[nt][i] = ex2_fast(x[nt][i]);
+          l[nt][i & 1] += x[nt][i];
+        }
+    };
+
+    auto add_to = [](float (&sum)[4], const float (&d)[4], float2 f01, float2 f23) {
+      const float2 p = fma2(make_float2(d[0], d[1]), f01, make_float2(sum[0], sum[1])), q = fma2(make_float2(d[2], d[3]), f23, make_float2(sum[2], sum[3]));
+      sum[0] = p.x; sum[1] = p.y; sum[2] = q.x; sum[3] = q.y;
+    };
+    // a tile of packed rows, UNITS times 16
+    auto packed_rows = [&](auto units, const unsigned char* base) {
+      constexpr int UNITS = decltype(units)::value;
+      float x[NT][4 * UNITS];
+      uint2 va[UNITS], vc[UNITS];
+      {
+        float d[UNITS][NT][2][4];
+        uint4 ka[UNITS], kc[UNITS];
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+          ka[u] = *reinterpret_cast<const uint4*>(base + u * Q4_UNIT_BYTES + lane * 16);
+          kc[u] = *reinterpret_cast<const uint4*>(base + u * Q4_UNIT_BYTES + 512 + lane * 16);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          uint32_t pa[UNITS][4], pc[UNITS][4];
+#pragma unroll
+          for (int u = 0; u < UNITS; ++u) {
+            q4_spread(word_of(ka[u], j), pa[u]);
+            q4_spread(word_of(kc[u], j), pc[u]);
+          }
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            const uint4 qw = q_half(nt, j);
+#pragma unroll
+            for (int u = 0; u < UNITS; ++u) {
+              const uint32_t A0[4] = {pa[u][0], pc[u][0], pa[u][1], pc[u][1]}, A1[4] = {pa[u][2], pc[u][2], pa[u][3], pc[u][3]};
+              if ((j & 1) == 0) mma_f16_first(d[u][nt][j >> 1], A0, qw.x, qw.y);
+              else mma_f16_next(d[u][nt][j >> 1], A0, qw.x, qw.y);
+              mma_f16_next(d[u][nt][j >> 1], A1, qw.z, qw.w);
             }
           }
-          // x = low + 16 s ((1 + c / 16) - 1): the sum over a group is 16 s (what the MMAs give) + (low - 16 s) (sum of q)
-          const float sa0 = 16.f * bf16lo(ha.x), sa1 = 16.f * bf16lo(ha.y), sc0 = 16.f * bf16lo(hc.x), sc1 = 16.f * bf16lo(hc.y);
-          const float za0 = bf16hi(ha.x) - sa0, za1 = bf16hi(ha.y) - sa1, zc0 = bf16hi(hc.x) - sc0, zc1 = bf16hi(hc.y) - sc1;
+        }
+        // x = low + s c: the sum over a group is s (what the MMAs give) + low (sum of q)
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+          const uint2 ha = *reinterpret_cast<const uint2*>(base + u * Q4_UNIT_BYTES + Q4_CODE_BYTES + g8 * 8), hc = *reinterpret_cast<const uint2*>(base + u * Q4_UNIT_BYTES + Q4_CODE_BYTES + 64 + g8 * 8);
+          const float sa0 = bf16lo(ha.x), sa1 = bf16lo(ha.y), sc0 = bf16lo(hc.x), sc1 = bf16lo(hc.y);
+          const float la0 = bf16hi(ha.x), la1 = bf16hi(ha.y), lc0 = bf16hi(hc.x), lc1 = bf16hi(hc.y);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-              x[nt][c] = (fmaf(d[nt][0][c], sa0, za0 * qsum[nt][0][c]) + fmaf(d[nt][1][c], sa1, za1 * qsum[nt][1][c])) * sl2;
-              x[nt][2 + c] = (fmaf(d[nt][0][2 + c], sc0, zc0 * qsum[nt][0][c]) + fmaf(d[nt][1][2 + c], sc1, zc1 * qsum[nt][1][c])) * sl2;
+              const float(&y)[2][4] = d[u][nt];
+              x[nt][4 * u + c] = fmaf(fmaf(y[0][c], sa0, y[1][c] * sa1), undo[nt][c], fmaf(la0, qsum[nt][0][c], fmaf(la1, qsum[nt][1][c], -ref[nt][c])));
+              x[nt][4 * u + 2 + c] = fmaf(fmaf(y[0][2 + c], sc0, y[1][2 + c] * sc1), undo[nt][c], fmaf(lc0, qsum[nt][0][c], fmaf(lc1, qsum[nt][1][c], -ref[nt][c])));
             }
-        }
-        weigh(x);
-        const uint2 va = *reinterpret_cast<const uint2*>(vb + Q4_CODE_BYTES + g8 * 8), vc = *reinterpret_cast<const uint2*>(vb + Q4_CODE_BYTES + 64 + g8 * 8);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          // values enter as (c - 8) / 16: x = (low + 8 s) + 16 s (c - 8) / 16
-          const uint32_t ga = h ? va.y : va.x, gc = h ? vc.y : vc.x;
-          const float s_a = 16.f * bf16lo(ga), s_c = 16.f * bf16lo(gc), z_a = fmaf(0.5f, s_a, bf16hi(ga)), z_c = fmaf(0.5f, s_c, bf16hi(gc));
-          uint32_t bh[NT][2], bl[NT][2];
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            planes(x[nt][0] * s_a, x[nt][1] * s_a, bh[nt][0], bl[nt][0]);
-            planes(x[nt][2] * s_c, x[nt][3] * s_c, bh[nt][1], bl[nt][1]);
-#pragma unroll
-            for (int c = 0; c < 2; ++c) zs[nt][h][c] = fmaf(x[nt][c], z_a, fmaf(x[nt][2 + c], z_c, zs[nt][h][c]));
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
-              bh[nt][y] = transpose_8x8(bh[nt][y]);
-              if (!SPLIT) bl[nt][y] = transpose_8x8(bl[nt][y]);
-            }
-          }
-          const uint4 vw = *reinterpret_cast<const uint4*>(vb + h * 512 + lane * 16);
-          const uint32_t w[4] = {vw.x, vw.y, vw.z, vw.w};
-#pragma unroll
-          for (int m = 0; m < 4; ++m) {
-            uint32_t A[4];
-            q4_spread(w[m], A);
-#pragma unroll
-            for (int y = 0; y < 4; ++y) A[y] = sub_bf16x2(A[y], 0x3fc03fc0u);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              mma_bf16_16816(acc[nt][4 * h + m], A, bh[nt][0], bh[nt][1]);
-              if (!SPLIT) mma_bf16_16816(acc[nt][4 * h + m], A, bl[nt][0], bl[nt][1]);
-            }
-          }
+          va[u] = *reinterpret_cast<const uint2*>(base + QA_V_OFF + u * Q4_UNIT_BYTES + Q4_CODE_BYTES + g8 * 8);
+          vc[u] = *reinterpret_cast<const uint2*>(base + QA_V_OFF + u * Q4_UNIT_BYTES + Q4_CODE_BYTES + 64 + g8 * 8);
         }
       }
-    } else {
-      // ================= bf16 rows: eight of them =================
-      const int jj = j < e2 ? j - e1 : j - e2;
-      const int rows = j < e2 ? QA_ROWS16 : min(QA_ROWS16, tail - jj * QA_ROWS16), pos = c_tail * v.C + jj * QA_ROWS16;      // (pos: of tail rows)
+      float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+      for (int u = 0; u < UNITS; ++u) {
+        s0 = fmaxf(s0, fmaxf(bf16lo(va[u].x), bf16lo(vc[u].x)));
+        s1 = fmaxf(s1, fmaxf(bf16lo(va[u].y), bf16lo(vc[u].y)));
+      }
+      weigh(x, s0, s1);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint32_t b[UNITS][NT][2];
+        uint4 vw[UNITS];
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+          const uint32_t ga = h ? va[u].y : va[u].x, gc = h ? vc[u].y : vc[u].x;
+          const float f_a = bf16lo(ga) * F[h], f_c = bf16lo(gc) * F[h], l_a = bf16hi(ga), l_c = bf16hi(gc);
+          vw[u] = *reinterpret_cast<const uint4*>(base + QA_V_OFF + u * Q4_UNIT_BYTES + h * 512 + lane * 16);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            const float* p = &x[nt][4 * u];
+            b[u][nt][0] = transpose_8x8(pack_f16x2(p[0] * f_a, p[1] * f_a));
+            b[u][nt][1] = transpose_8x8(pack_f16x2(p[2] * f_c, p[3] * f_c));
+#pragma unroll
+            for (int c = 0; c < 2; ++c) zs[nt][h][c] = fmaf(p[c], l_a, fmaf(p[2 + c], l_c, zs[nt][h][c]));
+          }
+        }
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+          float d[NT][4];
+#pragma unroll
+          for (int u = 0; u < UNITS; ++u) {
+            uint32_t A[4];
+            q4_spread(word_of(vw[u], m), A);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              if (u == 0) mma_f16_first(d[nt], A, b[u][nt][0], b[u][nt][1]);
+              else mma_f16_next(d[nt], A, b[u][nt][0], b[u][nt][1]);
+            }
+          }
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) add_to(acc[nt][4 * h + m], d[nt], make_float2(1.f, 1.f), make_float2(1.f, 1.f));
+        }
+      }
+    };
+
+    // a tile of `rows` <= 8 bf16 rows, the first at position pos
+    auto bf16_rows = [&](int rows, int pos, const unsigned char* base) {
       float x[NT][4];
       {
         float d[NT][2][4];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int y = 0; y < 4; ++y) d[nt][h][y] = 0.f;
-        const uint4* kr = reinterpret_cast<const uint4*>(base + qa_k_row(g8)) + t4;
+        const uint4* kr = reinterpret_cast<const uint4*>(base + g8 * ROW_BYTES) + t4;
 #pragma unroll
         for (int jw = 0; jw < 4; ++jw) {
           const uint4 kw = kr[4 * jw];
           const uint32_t A0[4] = {kw.x, 0u, kw.y, 0u}, A1[4] = {kw.z, 0u, kw.w, 0u};
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
-            const uint4 qw = Q_REGS ? qf[Q_REGS ? jw : 0] : *reinterpret_cast<const uint4*>(Qs + (nt * 8 + g8) * D + 32 * jw + 8 * t4);
-            mma_bf16_16816(d[nt][jw >> 1], A0, qw.x, qw.y);
-            mma_bf16_16816(d[nt][jw >> 1], A1, qw.z, qw.w);
+            const uint4 qw = *reinterpret_cast<const uint4*>(Qb + (nt * 8 + g8) * D + 32 * jw + 8 * t4);
+            if ((jw & 1) == 0) mma_bf16_first(d[nt][jw >> 1], A0, qw.x, qw.y);
+            else mma_bf16_next(d[nt][jw >> 1], A0, qw.x, qw.y);
+            mma_bf16_next(d[nt][jw >> 1], A1, qw.z, qw.w);
           }
         }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
-            const bool seen = g8 < rows && (j < e2 || pos + g8 <= last_pos[nt][c]);
-            x[nt][c] = seen ? (d[nt][0][c] + d[nt][1][c]) * sl2 : -INFINITY;
+            const bool seen = g8 < rows && pos + g8 <= last_pos(nt, c);
+            x[nt][c] = seen ? fmaf(d[nt][0][c] + d[nt][1][c], sl2, -ref[nt][c]) : -INFINITY;
             x[nt][2 + c] = -INFINITY;
           }
       }
-      weigh(x);
-      uint32_t bh[NT], bl[NT];
+      uint4 e[2], o[2];      // this lane's numbers of the rows 2 t4 and 2 t4 + 1
+      float largest[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        e[h] = *reinterpret_cast<const uint4*>(base + QA_V_OFF + 2 * t4 * ROW_BYTES + h * 128 + g8 * 16);
+        o[h] = *reinterpret_cast<const uint4*>(base + QA_V_OFF + (2 * t4 + 1) * ROW_BYTES + h * 128 + g8 * 16);
+        if (2 * t4 >= rows) e[h] = make_uint4(0u, 0u, 0u, 0u);      // what an earlier tile left there may be anything
+        if (2 * t4 + 1 >= rows) o[h] = make_uint4(0u, 0u, 0u, 0u);
+        auto larger = [](uint32_t p, uint32_t q) {
+          uint32_t d;
+          asm("max.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(p & 0x7fff7fffu), "r"(q & 0x7fff7fffu));
+          return d;
+        };
+        const uint32_t most = larger(larger(larger(e[h].x, e[h].y), larger(e[h].z, e[h].w)), larger(larger(o[h].x, o[h].y), larger(o[h].z, o[h].w)));
+        largest[h] = fmaxf(bf16lo(most), bf16hi(most)) * 0.125f;      // (as a scale: codes reach 8 from the middle)
+      }
+      weigh(x, largest[0], largest[1]);
+      // both planes of the weights in one MMA: rows 0-7 of its contraction have the first, rows 8-15, the same rows again, the second
+      uint32_t b[NT][2];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        planes(x[nt][0], x[nt][1], bh[nt], bl[nt]);
-        bh[nt] = transpose_8x8(bh[nt]);
-        if (!SPLIT) bl[nt] = transpose_8x8(bl[nt]);
+        const uint32_t hi = pack_bf16x2(x[nt][0], x[nt][1]);
+        b[nt][0] = transpose_8x8(hi);
+        b[nt][1] = transpose_8x8(pack_bf16x2(x[nt][0] - bf16lo(hi), x[nt][1] - bf16hi(hi)));
       }
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        uint4 e = *reinterpret_cast<const uint4*>(base + qa_v_row(2 * t4) + h * 128 + g8 * 16), o = *reinterpret_cast<const uint4*>(base + qa_v_row(2 * t4 + 1) + h * 128 + g8 * 16);
-        if (2 * t4 >= rows) e = make_uint4(0u, 0u, 0u, 0u);      // what an earlier tile left there may be anything
-        if (2 * t4 + 1 >= rows) o = make_uint4(0u, 0u, 0u, 0u);
-        const uint32_t ew[4] = {e.x, e.y, e.z, e.w}, ow[4] = {o.x, o.y, o.z, o.w};
+        const uint32_t ew[4] = {e[h].x, e[h].y, e[h].z, e[h].w}, ow[4] = {o[h].x, o[h].y, o[h].z, o[h].w};
+        const float f01 = F[h] * 0x1p-24f, f23 = F[h] * 0x1p-20f;
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
           const uint32_t a0 = __byte_perm(ew[m], ow[m], 0x5410), a1 = __byte_perm(ew[m], ow[m], 0x7632);
+          const uint32_t A[4] = {a0, a1, a0, a1};
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
-            mma_bf16_1688(acc[nt][4 * h + m], a0, a1, bh[nt]);
-            if (!SPLIT) mma_bf16_1688(acc[nt][4 * h + m], a0, a1, bl[nt]);
+            float d[4];
+            mma_bf16_first(d, A, b[nt][0], b[nt][1]);
+            add_to(acc[nt][4 * h + m], d, make_float2(f01, f01), make_float2(f23, f23));
           }
         }
       }
+    };
+
+    // leaves the state of the sequence in shared memory
+    auto leave = [&]() {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+          for (int o = 4; o <= 16; o <<= 1) {
+            l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], o);
+            zs[nt][0][c] += __shfl_xor_sync(0xffffffffu, zs[nt][0][c], o);
+            zs[nt][1][c] += __shfl_xor_sync(0xffffffffu, zs[nt][1][c], o);
+          }
+      const float un[2] = {1.f / F[0], 1.f / F[1]};
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          float* st = states + (warp * COLS + nt * 8 + 2 * t4 + c) * ATTN_PARTIAL_FLOATS;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const float zv = zs[nt][h][c];
+            float* o = st + 64 * h + 8 * g8;
+            float y[8];
+#pragma unroll
+            for (int m = 0; m < 4; ++m) {
+              y[2 * m] = fmaf(acc[nt][4 * h + m][c] * 0x1p24f, un[h], zv);
+              y[2 * m + 1] = fmaf(acc[nt][4 * h + m][2 + c] * 0x1p20f, un[h], zv);
+            }
+            *reinterpret_cast<float4*>(o) = make_float4(y[0], y[1], y[2], y[3]);
+            *reinterpret_cast<float4*>(o + 4) = make_float4(y[4], y[5], y[6], y[7]);
+          }
+          if (g8 == 0) { st[128] = over_by[nt][c] == -INFINITY ? -INFINITY : ref[nt][c]; st[129] = l[nt][c]; }
+        }
+      __syncwarp();
+    };
+
+    uint64_t *my_full = full + warp * STAGES, *my_empty = empty + warp * STAGES;
+    int nth = 0, stage = 0;      // sequences begun; stage of the next tile
+    uint32_t phase = 0;
+    bool ok = mbar_wait_bounded(fetched, 0);
+    if (!ok && lane == 0) set_status(v.status, ERR_TIMEOUT);
+    while (ok) {
+      if (!mbar_wait_bounded(&my_full[stage], phase)) {
+        if (lane == 0) set_status(v.status, ERR_TIMEOUT);
+        break;
+      }
+      const unsigned char* base = smem + (warp * STAGES + stage) * QA_TILE_BYTES;
+      const int4 what = infos[warp * STAGES + stage];
+      if (a.causal) n = progress[CW + 1];
+      if (what.w & QA_NEW) {      // its query rows were brought when the sequence two before it was merged, which this warp has waited for
+        start(nth & 1);
+        ++nth;
+      }
+      if (what.z == QA_ROWS4) packed_rows(std::integral_constant<int, 2>(), base);
+      else if (what.z > 0) packed_rows(std::integral_constant<int, 1>(), base);      // (the end of a chunk that is not a multiple of 32)
+      else if (what.z < 0) bf16_rows(-what.z, what.w >> 3, base);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&my_empty[stage]);
+      if (what.w & QA_FLUSH) {
+        // the states of the sequence before are done with
+        if (nth >= 2 && !mbar_wait_bounded(merged, (uint32_t)(nth - 2) & 1u)) {
+          if (lane == 0) set_status(v.status, ERR_TIMEOUT);
+          break;
+        }
+        leave();
+        if (what.w & QA_END) break;
+        if (lane == 0) mbar_arrive(left);      // release
+      }
+      if (++stage == STAGES) { stage = 0; phase ^= 1u; }
     }
-    __syncwarp();
-    if (i + STAGES < mine) issue(i + STAGES);
   }
 
-  // ---- the warps' states meet in shared memory ----
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-    for (int c = 0; c < 2; ++c)
-#pragma unroll
-      for (int o = 4; o <= 16; o <<= 1) {
-        l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], o);
-        zs[nt][0][c] += __shfl_xor_sync(0xffffffffu, zs[nt][0][c], o);
-        zs[nt][1][c] += __shfl_xor_sync(0xffffffffu, zs[nt][1][c], o);
+  // ---- the last sequence's states, by all warps; then sequences of which other CTAs have parts: the first and the last of this run ----
+  __syncthreads();
+  for (int r = warp; r < n_rows; r += WARPS) fold_states(x1, r);
+  __syncthreads();
+  // The ticket is an acquire-release atomic at device scope, taken when all warps have written their records: it publishes them, and makes those of the other
+  // CTAs visible to this one's warps once they have synchronised again.
+  if (threadIdx.x < 2) {
+    const int x = threadIdx.x ? x1 : x0;
+    const int parts = (int)(qa_owner((uint32_t)(x + 1) * uk - 1u, n_items, P) - qa_owner((uint32_t)x * uk, n_items, P)) + 1;
+    int mine = 0;
+    if (parts > 1 && (threadIdx.x == 0 || x1 > x0)) {
+      int arrived;
+      asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(arrived) : "l"(a.counters + x * a.groups + group) : "memory");
+      if (arrived == parts - 1) {
+        mine = parts;
+        a.counters[x * a.groups + group] = 0;      // clean for the next launch
       }
-  if constexpr (SPLIT) {      // the two planes
-#pragma unroll
-    for (int m = 0; m < 8; ++m)
-#pragma unroll
-      for (int x = 0; x < 4; ++x) acc[0][m][x] += __shfl_xor_sync(0xffffffffu, acc[0][m][x], 2);
+    }
+    flags[threadIdx.x] = mine;
   }
-  __syncthreads();      // every warp's last tile has been read
-  float* states = reinterpret_cast<float*>(smem);      // [warp][column][132]
-  if (!SPLIT || t4 < 2) {
+  __syncthreads();
+  for (int e = 0; e < 2; ++e) {
+    const int parts = flags[e], x = e ? x1 : x0;
+    if (parts == 0) continue;
+    const float* recs = a.partials + ((long long)(x + (int)qa_owner((uint32_t)x * uk, n_items, P)) * a.groups + group) * COLS * ATTN_PARTIAL_FLOATS;
+    const long long stride = (long long)a.groups * COLS * ATTN_PARTIAL_FLOATS;      // from run to run
+    // several warps share the records of a row where there are fewer rows than warps; a record is one trip to L2
+    const int per_row = n_rows >= WARPS ? 1 : WARPS / n_rows;
+    for (int y = warp; y < n_rows * per_row; y += WARPS) {
+      const int r = y / per_row, sub = y - r * per_row;
+      const float* rec = recs + r * ATTN_PARTIAL_FLOATS;
+      float top = -INFINITY, sum = 0.f;
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int p0 = sub; p0 < parts; p0 += 4 * per_row) {
+        float m[4], l[4];
+        float4 w[4];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        float* st = states + ((warp * Shape::COLS) + nt * 8 + 2 * t4 + c) * ATTN_PARTIAL_FLOATS;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const float zv = zs[nt][h][c];
-          float* o = st + 64 * h + 8 * g8;
-          *reinterpret_cast<float4*>(o) = make_float4(acc[nt][4 * h][c] + zv, acc[nt][4 * h][2 + c] + zv, acc[nt][4 * h + 1][c] + zv, acc[nt][4 * h + 1][2 + c] + zv);
-          *reinterpret_cast<float4*>(o + 4) = make_float4(acc[nt][4 * h + 2][c] + zv, acc[nt][4 * h + 2][2 + c] + zv, acc[nt][4 * h + 3][c] + zv, acc[nt][4 * h + 3][2 + c] + zv);
+        for (int i = 0; i < 4; ++i) {
+          const int p = p0 + i * per_row;
+          const float* st = rec + (p < parts ? p : p0) * stride;
+          m[i] = __ldcg(st + 128); l[i] = __ldcg(st + 129);
+          w[i] = __ldcg(reinterpret_cast<const float4*>(st + lane * 4));
         }
-        if (g8 == 0) { st[128] = ref[nt][c]; st[129] = l[nt][c]; }
+        float to = top;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) to = fmaxf(to, m[i]);
+        const float f0 = top == -INFINITY ? 0.f : exp2f(top - to);
+        sum *= f0; o.x *= f0; o.y *= f0; o.z *= f0; o.w *= f0;
+        top = to;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (p0 + i * per_row >= parts) continue;
+          const float f = m[i] == -INFINITY ? 0.f : exp2f(m[i] - top);
+          sum = fmaf(l[i], f, sum);
+          o.x = fmaf(w[i].x, f, o.x); o.y = fmaf(w[i].y, f, o.y); o.z = fmaf(w[i].z, f, o.z); o.w = fmaf(w[i].w, f, o.w);
+        }
       }
-  }
-  if (threadIdx.x == 0) *flag = 0;
-  __syncthreads();
-  auto finish = [&](int rr, float4 o, float top, float sum) {      // a warp writes query row rr
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;                // (no row, or weights of 0 only: 0; NaN stays)
-    const int t = (int)a.by_g.div((uint32_t)rr), g = rr - t * a.G, b = s / v.H, h = s - b * v.H;
-    const long long at = (((long long)b * a.T + t) * v.H + h) * a.G + g;
-    *reinterpret_cast<uint2*>(a.out + at * D + lane * 4) = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
-    if (a.lse && lane == 0) a.lse[at] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.69314718055994530942f;
-  };
-  for (int r = warp; r < n_rows; r += QA_WARPS) {
-    const float* st = states + r * ATTN_PARTIAL_FLOATS;
-    constexpr int STRIDE = Shape::COLS * ATTN_PARTIAL_FLOATS;
-    float top = -INFINITY, sum = 0.f;
-#pragma unroll
-    for (int w = 0; w < QA_WARPS; ++w) top = fmaxf(top, st[w * STRIDE + 128]);
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int w = 0; w < QA_WARPS; ++w) {
-      const float m = st[w * STRIDE + 128], f = m == -INFINITY ? 0.f : exp2f(m - top);
-      const float4 x = *reinterpret_cast<const float4*>(st + w * STRIDE + lane * 4);
-      sum = fmaf(st[w * STRIDE + 129], f, sum);
-      o.x = fmaf(x.x, f, o.x); o.y = fmaf(x.y, f, o.y); o.z = fmaf(x.z, f, o.z); o.w = fmaf(x.w, f, o.w);
+      if (per_row == 1) {
+        write_row(a, x, row0 + r, o, top, sum, lane);
+      } else {
+        float* st = states + y * ATTN_PARTIAL_FLOATS;
+        *reinterpret_cast<float4*>(st + lane * 4) = o;
+        if (lane == 0) { st[128] = top; st[129] = sum; }
+      }
     }
-    if (a.splits == 1) {
-      finish(row0 + r, o, top, sum);
-    } else {
-      float* rec = a.partials + (((long long)s * a.splits + part) * R + row0 + r) * ATTN_PARTIAL_FLOATS;
-      *reinterpret_cast<float4*>(rec + lane * 4) = o;
-      if (lane == 0) { rec[128] = top; rec[129] = sum; }
+    if (per_row > 1) {
+      __syncthreads();
+      for (int r = warp; r < n_rows; r += WARPS) {
+        const float* st = states + r * per_row * ATTN_PARTIAL_FLOATS;
+        float top = -INFINITY, sum = 0.f;
+        for (int sub = 0; sub < per_row; ++sub) top = fmaxf(top, st[sub * ATTN_PARTIAL_FLOATS + 128]);
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int sub = 0; sub < per_row; ++sub) fold(st + sub * ATTN_PARTIAL_FLOATS, top, sum, o, lane);
+        write_row(a, x, row0 + r, o, top, sum, lane);
+      }
     }
+    __syncthreads();
   }
-  if (a.splits == 1) return;
-  __threadfence();
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    int arrived;
-    asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(arrived) : "l"(a.counters + (long long)z * v.S + s) : "memory");
-    *flag = arrived == a.splits - 1 ? 1 : 0;
-  }
-  __syncthreads();
-  if (*flag == 0) return;
-  __threadfence();
-  for (int r = warp; r < n_rows; r += QA_WARPS) {
-    const float* rec = a.partials + ((long long)s * a.splits * R + row0 + r) * ATTN_PARTIAL_FLOATS;
-    const long long stride = (long long)R * ATTN_PARTIAL_FLOATS;
-    float top = -INFINITY, sum = 0.f;
-    for (int p = lane; p < a.splits; p += 32) top = fmaxf(top, __ldcg(rec + p * stride + 128));
-    top = warp_max(top);
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-    for (int p = 0; p < a.splits; ++p) {
-      const float m = __ldcg(rec + p * stride + 128), lp = __ldcg(rec + p * stride + 129);
-      const float4 x = __ldcg(reinterpret_cast<const float4*>(rec + p * stride + lane * 4));
-      const float f = m == -INFINITY ? 0.f : exp2f(m - top);
-      sum = fmaf(lp, f, sum);
-      o.x = fmaf(x.x, f, o.x); o.y = fmaf(x.y, f, o.y); o.z = fmaf(x.z, f, o.z); o.w = fmaf(x.w, f, o.w);
-    }
-    finish(row0 + r, o, top, sum);
-  }
-  if (threadIdx.x == 0) a.counters[(long long)z * v.S + s] = 0;      // clean for the next launch
 }
 
-int q4_attn_row_groups(int rows) { return rows <= 16 ? 1 : (rows + 31) / 32; }
+Q4AttnShape q4_attn_shape(int rows) {
+  const int cols = rows <= QaShape<1>::COLS ? QaShape<1>::COLS : QaShape<2>::COLS;
+  return {cols, (rows + cols - 1) / cols};
+}
 
-cudaError_t launch_attn_q4(const LayerView& v, const Q4Pages& p, bool dense, int T, int G, bool causal, int splits, const void* q, void* out, float* lse,
-                           float scale, float* partials, int32_t* counters, cudaStream_t st) {
+cudaError_t launch_attn_q4(const LayerView& v, const Q4Pages& p, bool dense, int T, int G, bool causal, int parts_per_seq, int runs, const void* q, void* out,
+                           float* lse, float scale, float* partials, int32_t* counters, cudaStream_t st) {
+  const Q4AttnShape shape = q4_attn_shape(T * G);
   Q4AttnArgs a;
   a.v = v; a.p = p;
-  a.by_g = fast_div((uint32_t)G);
+  a.by_g = fast_div((uint32_t)G); a.by_h = fast_div((uint32_t)v.H); a.by_k = fast_div((uint32_t)parts_per_seq);
   a.by_tiles4 = fast_div((uint32_t)((v.C + QA_ROWS4 - 1) / QA_ROWS4));
   a.by_tiles16 = fast_div((uint32_t)(v.C / QA_ROWS16));
-  a.dense = dense ? 1 : 0; a.T = T; a.G = G; a.causal = causal ? 1 : 0; a.splits = splits;
+  a.dense = dense ? 1 : 0; a.T = T; a.G = G; a.causal = causal ? 1 : 0; a.k = parts_per_seq; a.groups = shape.groups;
   a.q = static_cast<const uint16_t*>(q); a.out = static_cast<uint16_t*>(out); a.lse = lse; a.scale = scale;
   a.partials = partials; a.counters = counters;
-  const int R = T * G;
-  const dim3 grid((unsigned)splits, (unsigned)v.S, (unsigned)q4_attn_row_groups(R));
-  auto launch = [&](auto kernel, DeviceFlags& opted, int smem) {
+  auto launch = [&](auto kernel, DeviceFlags& opted, int warps, int smem) {
     const cudaError_t e = smem_opt_in(opted, kernel, smem);
-    return e != cudaSuccess ? e : launch_pdl(kernel, grid, dim3(QA_WARPS * 32), (size_t)smem, st, a);
+    return e != cudaSuccess ? e : launch_pdl(kernel, dim3((unsigned)(runs * shape.groups)), dim3((unsigned)warps * 32), (size_t)smem, st, a);
   };
-  static DeviceFlags f4, f8, f16, f32;
-  if (R <= 4) return launch(kve_decode_attn_q4_kernel<1, true>, f4, QaShape<1>::SMEM);
-  if (R <= 8) return launch(kve_decode_attn_q4_kernel<1, false>, f8, QaShape<1>::SMEM);
-  if (R <= 16) return launch(kve_decode_attn_q4_kernel<2, false>, f16, QaShape<2>::SMEM);
-  return launch(kve_decode_attn_q4_kernel<4, false>, f32, QaShape<4>::SMEM);
+  static DeviceFlags f8, f16;
+  if (shape.cols == QaShape<1>::COLS) return launch(kve_decode_attn_q4_kernel<1>, f8, QaShape<1>::WARPS, QaShape<1>::SMEM);
+  return launch(kve_decode_attn_q4_kernel<2>, f16, QaShape<2>::WARPS, QaShape<2>::SMEM);
 }
 
 }  // namespace kve

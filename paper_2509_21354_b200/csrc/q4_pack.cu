@@ -115,7 +115,7 @@ __global__ void __launch_bounds__(PK_WARPS * 32) kve_pack_kernel(LayerView v, Q4
       codes[warp][line * PK_PITCH + l16] = __byte_perm(q4_half(c[0], c[1], c[2], c[3]), q4_half(c[4], c[5], c[6], c[7]), 0x5410);
     } else {
       const uint32_t w = __byte_perm(q4_half(c[0], c[2], c[4], c[6]), q4_half(c[1], c[3], c[5], c[7]), 0x5410);
-      *reinterpret_cast<uint32_t*>(dst + line * 64 + (l16 & 3) * 16 + (l16 >> 2) * 4) = q4_turn(w);
+      *reinterpret_cast<uint32_t*>(dst + line * 64 + (l16 & 3) * 16 + (l16 >> 2) * 4) = w;
     }
     if ((l16 & 7) == 0)
       *reinterpret_cast<uint32_t*>(dst + Q4_CODE_BYTES + line * 8 + (l16 >> 3) * 4) = sb | (sb == 0x7fffu ? 0x7fff0000u : (__float_as_uint(g.low) & 0xffff0000u));
@@ -128,7 +128,7 @@ __global__ void __launch_bounds__(PK_WARPS * 32) kve_pack_kernel(LayerView v, Q4
     for (int h = 0; h < 2; ++h) {
       uint32_t w[4] = {cw[8 * h], cw[8 * PK_PITCH + 8 * h], cw[PK_PITCH + 8 * h], cw[9 * PK_PITCH + 8 * h]};
       transpose_bytes(w);
-      *reinterpret_cast<uint4*>(dst + h * 512 + lane * 16) = make_uint4(q4_turn(w[0]), q4_turn(w[1]), q4_turn(w[2]), q4_turn(w[3]));
+      *reinterpret_cast<uint4*>(dst + h * 512 + lane * 16) = make_uint4(w[0], w[1], w[2], w[3]);
     }
   }
 }
@@ -159,7 +159,7 @@ __global__ void __launch_bounds__(PK_WARPS * 32) kve_unpack_kernel(LayerView v, 
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const uint4 q = __ldcs(reinterpret_cast<const uint4*>(src + h * 512 + lane * 16));
-    uint32_t w[4] = {q4_unturn(q.x), q4_unturn(q.y), q4_unturn(q.z), q4_unturn(q.w)};
+    uint32_t w[4] = {q.x, q.y, q.z, q.w};
     const int g8 = lane >> 2, t4 = lane & 3;
     if (is_v) {
       transpose_bytes(w);
