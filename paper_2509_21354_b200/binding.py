@@ -80,8 +80,8 @@ _bind = None
 
 
 def _load_bind(build_if_missing: bool):
-    """The extension module behind Store.decode_step (csrc/bind.cpp).  Where it cannot be built or loaded (no compiler, no
-    headers) that one call goes through ctypes like all others, 2 us slower."""
+    """The extension module behind the calls of a decode loop (csrc/bind.cpp).  Where it cannot be built or loaded (no compiler, no
+    headers) they go through ctypes like all others, 2 us and more slower."""
     global _bind
     if _bind is None:
         try:
@@ -89,6 +89,7 @@ def _load_bind(build_if_missing: bool):
             spec = importlib.util.spec_from_file_location("_kve_bind", path)
             module = importlib.util.module_from_spec(spec)
             spec.loader.exec_module(module)
+            module.append_rope      # (an older module has no such call)
             _bind = module
         except Exception as e:
             warnings.warn(f"the decode step's extension module is not available ({e}); calling through ctypes")
@@ -254,6 +255,7 @@ class Rope:
         if len(axis) != 64 or len(freq) != 64 or min(axis) < 0 or not 1 <= self.n_axes <= 4:
             raise ValueError("64 pairs, 1 to 4 axes")
         self.c = kvE_rope(n_axes=self.n_axes, layout=ROPE_LAYOUT[layout], axis=(C.c_uint8 * 64)(*axis), inv_freq=(C.c_double * 64)(*freq))
+        self.address = C.addressof(self.c)
 
 
 class Store:
@@ -272,6 +274,8 @@ class Store:
         self.lib = load_library()
         self._decode_step = _bind.decode_step if _bind is not None else None
         self._decode_step_fn = C.cast(self.lib.kvE_decode_step, C.c_void_p).value
+        self._address = {name: C.cast(getattr(self.lib, name), C.c_void_p).value
+                         for name in ("kvE_append_rope", "kvE_append_rope_next", "kvE_decode_attn_q4", "kvE_pack_chunks", "kvE_unpack_chunks", "kvE_set_len")}
         self.device = torch.device(device)
         self.Hq = H if Hq is None else Hq
         self.cfg = kvE_config(B=B, Hq=self.Hq, Hkv=H, d=128, C=C_, W=W, max_tokens=max_tokens, n_layers=n_layers,
@@ -455,7 +459,12 @@ class Store:
 
     def pack_chunks(self, layer, chunk_begin, chunk_end, stream=None):
         """chunks outside the window to 4 bits"""
-        _check("kvE_pack_chunks", self.lib.kvE_pack_chunks(self.handle, layer, int(chunk_begin), int(chunk_end), _stream(self, stream)), self.handle)
+        if _bind is None:
+            rc = self.lib.kvE_pack_chunks(self.handle, layer, int(chunk_begin), int(chunk_end), _stream(self, stream))
+        else:
+            rc = _bind.chunks(*_native(self, "kvE_pack_chunks", stream), layer, chunk_begin, chunk_end)
+        if rc:
+            _check("kvE_pack_chunks", rc, self.handle)
 
     def unpack_chunks(self, layer, chunk_begin, chunk_end, k_out=None, v_out=None, stream=None):
         return kvE_unpack_chunks(self, layer, chunk_begin, chunk_end, k_out, v_out, stream)
@@ -495,8 +504,18 @@ def kvE_append(st: Store, layer, k_new, v_new, stream=None) -> int:
     return ready.value
 
 
+def _native(st, name, stream) -> tuple:
+    """the first arguments of a call of the extension module: function, handle, device, stream"""
+    return st._address[name], st.handle and st.handle.value, st.device_index, None if stream is None else stream.cuda_stream
+
+
 def kvE_set_len(st: Store, layer, n, stream=None):
-    _check("kvE_set_len", st.lib.kvE_set_len(st.handle, layer, int(n), _stream(st, stream)), st.handle)
+    if _bind is None:
+        rc = st.lib.kvE_set_len(st.handle, layer, int(n), _stream(st, stream))
+    else:
+        rc = _bind.set_len(*_native(st, "kvE_set_len", stream), layer, n)
+    if rc:
+        _check("kvE_set_len", rc, st.handle)
 
 
 def kvE_summarize_chunks(st: Store, layer, chunk_begin, chunk_end, agg_weights=None, stream=None):
@@ -583,6 +602,11 @@ def kvE_append_rope(st: Store, layer, q, k_new, v_new, rope, positions=None, q_o
     """q: bf16 [B, n_new, Hq, 128] or None; k_new, v_new: bf16 [B, n_new, Hkv, 128]; rows contiguous, otherwise any strides (parts of
     one projection's output).  positions: int32 [B, n_new, n_axes], or None: the index in the cache on every axis.
     Returns (q_out, number of chunks ready to gate)."""
+    if _bind is not None:
+        rc, q_out, ready = _bind.append_rope(*_native(st, "kvE_append_rope", stream), 0, layer, st.B, st.Hq, st.H, 0, q, k_new, v_new, rope.address, positions, q_out)
+        if rc:
+            _check("kvE_append_rope", rc, st.handle)
+        return q_out, ready
     rows, k, v, pos, n, q_out = _rope_arguments(st, q, k_new, v_new, rope, positions, q_out)
     ready = C.c_int(0)
     _check("kvE_append_rope", st.lib.kvE_append_rope(st.handle, layer, rows, k, v, pos, n, C.byref(rope.c), _p(q_out), C.byref(ready), _stream(st, stream)),
@@ -591,6 +615,11 @@ def kvE_append_rope(st: Store, layer, q, k_new, v_new, rope, positions=None, q_o
 
 
 def kvE_append_rope_next(st: Store, layer, q, k_new, v_new, rope, positions=None, q_out=None, n_reserve=0, stream=None):
+    if _bind is not None:
+        rc, q_out, _ = _bind.append_rope(*_native(st, "kvE_append_rope_next", stream), 1, layer, st.B, st.Hq, st.H, n_reserve, q, k_new, v_new, rope.address, positions, q_out)
+        if rc:
+            _check("kvE_append_rope_next", rc, st.handle)
+        return q_out
     rows, k, v, pos, n, q_out = _rope_arguments(st, q, k_new, v_new, rope, positions, q_out)
     _check("kvE_append_rope_next", st.lib.kvE_append_rope_next(st.handle, layer, rows, k, v, pos, n, int(n_reserve), C.byref(rope.c), _p(q_out),
                                                                _stream(st, stream)), st.handle)
@@ -599,6 +628,11 @@ def kvE_append_rope_next(st: Store, layer, q, k_new, v_new, rope, positions=None
 
 def kvE_unpack_chunks(st: Store, layer, chunk_begin, chunk_end, k_out=None, v_out=None, stream=None):
     """What the packed chunks stand for: bf16 [S, (chunk_end - chunk_begin) C, 128], keys and values."""
+    if _bind is not None:
+        rc, k_out, v_out = _bind.unpack_chunks(*_native(st, "kvE_unpack_chunks", stream), layer, chunk_begin, chunk_end, st.S, st.C, k_out, v_out)
+        if rc:
+            _check("kvE_unpack_chunks", rc, st.handle)
+        return k_out, v_out
     shape = (st.S, max(0, int(chunk_end) - int(chunk_begin)) * st.C, 128)
     k_out, v_out = (torch.empty(shape, dtype=_BF16, device=st.device) if t is None else t for t in (k_out, v_out))
     if shape[1] > 0:      # (an empty tensor has no address)
@@ -609,6 +643,11 @@ def kvE_unpack_chunks(st: Store, layer, chunk_begin, chunk_end, k_out=None, v_ou
 
 def kvE_decode_attn_q4(st: Store, layer, q, dense=False, causal=False, out=None, lse=None, scale=None, stream=None):
     """q: bf16 [B, T, Hq, 128] device tensor.  Returns out (same shape); lse, if given, is an fp32 [B, T, Hq] device tensor."""
+    if _bind is not None:
+        rc, out = _bind.decode_attn_q4(*_native(st, "kvE_decode_attn_q4", stream), layer, st.B, st.Hq, dense, causal, _DEFAULT_SCALE if scale is None else scale, q, out, lse)
+        if rc:
+            _check("kvE_decode_attn_q4", rc, st.handle)
+        return out
     assert q.dtype is _BF16 and q.dim() == 4 and q.shape[0] == st.B and q.shape[2:] == (st.Hq, 128)
     if out is None:
         out = torch.empty_like(q)

@@ -33,7 +33,7 @@ def bind_path() -> str:
 def build_bind(force: bool = False) -> str:
     """Compiles csrc/bind.cpp (an extension module against this interpreter and this torch; no device code)."""
     src, BIND = os.path.join(CSRC, "bind.cpp"), bind_path()
-    if not force and os.path.exists(BIND) and os.path.getmtime(BIND) >= os.path.getmtime(src):
+    if not force and os.path.exists(BIND) and os.path.getmtime(BIND) >= max(os.path.getmtime(f) for f in (src, os.path.join(HERE, "..", "include", "kve.h"))):
         return BIND
     import sysconfig
     import torch
