@@ -8,6 +8,8 @@
 // (x - low and s have few bits: one number in 250 of a normal distribution).  rint((x - low) / s - 2^-12) is the code or one less, as the
 // quotient's own error is below 2^-18, and the remainder x - low - c s says which: x - low is rounded up, so that it is above a border
 // (which fp32 holds) exactly where the real difference is, and the remainder of that is exact.
+#include <type_traits>
+
 #include "q4.cuh"
 
 namespace kve {
@@ -49,19 +51,19 @@ __device__ __forceinline__ uint32_t q4_scale_bits(float high, float low) {
   return (u + 0x7fffu + ((u >> 16) & 1u)) >> 16;
 }
 
-// The codes of eight numbers of a group (c[i]: whole numbers 0..15)
-struct Q4Group { float low, scale; };
-__device__ __forceinline__ void q4_codes(const uint4& x, const Q4Group& g, float (&c)[8]) {
-  // tiny scales are taken 2^64 times as large, so that 1 / scale stays finite; scale 0: all codes 0
-  const float up = g.scale > 0.f && g.scale < 0x1p-60f ? 0x1p64f : 1.f;
-  const float s = g.scale * up, inv = s > 0.f ? __frcp_rn(s) : 0.f, half = s > 0.f ? 0.5f * s : INFINITY;
-  const float2 up2 = make_float2(up, up), off = make_float2(-g.low * up, -g.low * up), inv2 = make_float2(inv, inv), neg_s = make_float2(-s, -s);
+// The codes of eight numbers of a group (c[i]: whole numbers 0..15).  TINY: scales may be so small that 1 / scale overflows: those are taken 2^64 times as large.
+template <bool TINY>
+__device__ __forceinline__ void q4_codes(const uint4& x, float scale, float low, float inv, float (&c)[8]) {
+  const float up = TINY && scale < 0x1p-60f ? 0x1p64f : 1.f;
+  const float s = TINY ? scale * up : scale, half = 0.5f * s;      // (scale 0: the codes do not matter)
+  if (TINY) inv = s > 0.f ? __frcp_rn(s) : 0.f;
+  const float2 up2 = make_float2(up, up), off = make_float2(-low * up, -low * up), inv2 = make_float2(inv, inv), neg_s = make_float2(-s, -s);
   const float2 eps = make_float2(-0x1p-12f, -0x1p-12f), magic = make_float2(0x1.8p23f, 0x1.8p23f), unmagic = make_float2(-0x1.8p23f, -0x1.8p23f);
   const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const float2 t = fma2_up(make_float2(bf16lo(w[e]), bf16hi(w[e])), up2, off);      // x - low
-    float2 n = add2(add2(fma2(t, inv2, eps), magic), unmagic);                     // the code, or one less
+    float2 n = add2(add2(fma2(t, inv2, eps), magic), unmagic);                        // the code, or one less
     const float2 r = fma2(n, neg_s, t);
     if (r.x > half) n.x += 1.f;
     if (r.y > half) n.y += 1.f;
@@ -97,29 +99,44 @@ __global__ void __launch_bounds__(PK_WARPS * 32) kve_pack_kernel(LayerView v, Q4
   uint4 row[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) row[i] = __ldcs(src + i * 32);      // rows 2 i + half
+  // (largest, -smallest) of this lane's part of row 2 i + half; then of the whole group, lane by lane: lane 8 g + i has group g of the rows 2 i and 2 i + 1
+  uint32_t m[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const uint4& r = row[i];
     const uint32_t mx = max2_nan(max2_nan(r.x, r.y), max2_nan(r.z, r.w)), mn = min2_nan(min2_nan(r.x, r.y), min2_nan(r.z, r.w)) ^ 0x80008000u;
-    uint32_t m = max2_nan(__byte_perm(mx, mn, 0x5410), __byte_perm(mx, mn, 0x7632));      // (largest, -smallest)
-#pragma unroll
-    for (int o = 1; o <= 4; o <<= 1) m = max2_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
-    Q4Group g;
-    g.low = -bf16hi(m);
-    const uint32_t sb = q4_scale_bits(bf16lo(m), g.low);
-    g.scale = __uint_as_float(sb << 16);
-    float c[8];
-    q4_codes(r, g, c);
-    const int line = 2 * i + half;
-    if (is_v) {
-      codes[warp][line * PK_PITCH + l16] = __byte_perm(q4_half(c[0], c[1], c[2], c[3]), q4_half(c[4], c[5], c[6], c[7]), 0x5410);
-    } else {
-      const uint32_t w = __byte_perm(q4_half(c[0], c[2], c[4], c[6]), q4_half(c[1], c[3], c[5], c[7]), 0x5410);
-      *reinterpret_cast<uint32_t*>(dst + line * 64 + (l16 & 3) * 16 + (l16 >> 2) * 4) = w;
-    }
-    if ((l16 & 7) == 0)
-      *reinterpret_cast<uint32_t*>(dst + Q4_CODE_BYTES + line * 8 + (l16 >> 3) * 4) = sb | (sb == 0x7fffu ? 0x7fff0000u : (__float_as_uint(g.low) & 0xffff0000u));
+    m[i] = max2_nan(__byte_perm(mx, mn, 0x5410), __byte_perm(mx, mn, 0x7632));
   }
+#pragma unroll
+  for (int o = 4; o >= 1; o >>= 1) {
+    const bool upper = lane & o;
+#pragma unroll
+    for (int i = 0; i < o; ++i) {
+      const uint32_t keep = upper ? m[i + o] : m[i], give = upper ? m[i] : m[i + o];
+      m[i] = max2_nan(keep, __shfl_xor_sync(0xffffffffu, give, o));
+    }
+  }
+  const uint32_t sb = q4_scale_bits(bf16lo(m[0]), -bf16hi(m[0])), head = sb | (sb == 0x7fffu ? 0x7fff0000u : (m[0] & 0xffff0000u) ^ 0x80000000u);
+  const float my_scale = __uint_as_float(sb << 16), my_inv = my_scale > 0.f ? __frcp_rn(my_scale) : 0.f;
+  *reinterpret_cast<uint32_t*>(dst + Q4_CODE_BYTES + (2 * (lane & 7) + half) * 8 + ((lane >> 3) & 1) * 4) = head;
+  auto encode = [&](auto tiny) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int from = (lane & 24) | i, line = 2 * i + half;
+      const uint32_t g = __shfl_sync(0xffffffffu, head, from);
+      const float inv = __shfl_sync(0xffffffffu, my_inv, from);
+      float c[8];
+      q4_codes<decltype(tiny)::value>(row[i], bf16lo(g), bf16hi(g), inv, c);
+      if (is_v) {
+        codes[warp][line * PK_PITCH + l16] = __byte_perm(q4_half(c[0], c[1], c[2], c[3]), q4_half(c[4], c[5], c[6], c[7]), 0x5410);
+      } else {
+        const uint32_t w = __byte_perm(q4_half(c[0], c[2], c[4], c[6]), q4_half(c[1], c[3], c[5], c[7]), 0x5410);
+        *reinterpret_cast<uint32_t*>(dst + line * 64 + (l16 & 3) * 16 + (l16 >> 2) * 4) = w;
+      }
+    }
+  };
+  if (__any_sync(0xffffffffu, my_scale > 0.f && my_scale < 0x1p-100f)) encode(std::true_type());
+  else encode(std::false_type());
   if (is_v) {
     __syncwarp();
     const int g8 = lane >> 2, t4 = lane & 3;

@@ -14,6 +14,7 @@
 namespace kve {
 
 constexpr int RP_THREADS = 256;
+constexpr int RP_CTAS = 6;                    // per SM (with four tokens each; 5 of them 273 us, 4 285)
 constexpr int RP_ROWS = RP_THREADS / 8;       // rows under way at a time
 constexpr int RP_MAX_TOKENS = 8;              // tokens of one CTA (few heads)
 constexpr int RP_TABLE = 8 * 9;               // (cos, sin) of pair 8 x + e at 9 x + e: eight threads read different banks
@@ -25,7 +26,7 @@ struct RopeArgs : RopeCall {
 
 // NEXT: at the length the device holds, which the last CTA advances (as kve_append_next_kernel does)
 template <bool NEXT>
-__global__ void __launch_bounds__(RP_THREADS) kve_append_rope_kernel(LayerView v, RopeArgs a) {
+__global__ void __launch_bounds__(RP_THREADS, RP_CTAS) kve_append_rope_kernel(LayerView v, RopeArgs a) {
   __shared__ float2 table[RP_MAX_TOKENS][RP_TABLE];
   __shared__ int last;
   pdl_launch_dependents();
@@ -153,7 +154,11 @@ cudaError_t launch_append_rope(const LayerView& v, const RopeCall& call, bool ne
   RopeArgs a;
   static_cast<RopeCall&>(a) = call;
   a.n_tokens = v.B * a.n_new;
-  int per = RP_ROWS / rows;      // one pass of the CTA, or one token
+  // one pass of the CTA, or one token; with tokens for two full waves, up to four (the angles of four tokens take as long as those of one: 8 x 4096 tokens of
+  // 96 rows 396 us with one token a CTA, 301 with two, 269 with four, 276 with eight)
+  int per = RP_ROWS / rows, most = a.n_tokens / (2 * RP_CTAS * sm_count());
+  if (most > 4) most = 4;
+  per = per < most ? most : per;
   per = per < 1 ? 1 : (per > RP_MAX_TOKENS ? RP_MAX_TOKENS : per);
   a.tokens_per_cta = per;
   a.by_rows = fast_div((uint32_t)rows); a.by_new = fast_div((uint32_t)a.n_new); a.by_c = fast_div((uint32_t)v.C);
