@@ -320,12 +320,11 @@ int kvE_append_rope_next(kvE_store* st, int layer, const kvE_rows* q, const kvE_
  * Chunks [0, n_packed) of a layer have such a copy (kvE_packed_chunks); n_packed is held on the device too.  kvE_set_len to a length that cuts
  * into them lowers it to the chunks that are still complete; a caller who writes pages himself sets the length to 0 first. */
 #define KVE_Q4_UNIT_ROWS 16       /* C must be a multiple of it */
-#define KVE_Q4_UNIT_BYTES 1152    /* of 16 rows: codes and scales */
+#define KVE_Q4_UNIT_BYTES 2304    /* of 16 keys and 16 values: codes and scales */
 typedef struct {
-  void* k4_pages;         /* [n_pages4][C / 16][KVE_Q4_UNIT_BYTES], on 16 bytes; one page = one chunk of one (layer, b, h) */
-  void* v4_pages;
+  void* kv4_pages;        /* [n_pages4][C / 16][KVE_Q4_UNIT_BYTES], on 16 bytes; one page = one chunk of one (layer, b, h), keys and values */
   int64_t n_pages4;
-  const int32_t* page_table4;   /* [n_layers][S][max_chunks] page ids in these pools, filled by the caller */
+  const int32_t* page_table4;   /* [n_layers][S][max_chunks] page ids in this pool, filled by the caller */
   int32_t max_query_tokens;     /* most query tokens per kvE_decode_attn_q4 call, times Hq / Hkv at most 128 */
   void* workspace;        /* kvE_q4_workspace_bytes bytes, 256-byte aligned, cleared by kvE_attach_q4 */
   size_t workspace_bytes;

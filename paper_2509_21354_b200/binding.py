@@ -69,11 +69,11 @@ class kvE_rows(C.Structure):
 
 
 class kvE_q4_buffers(C.Structure):
-    _fields_ = [("k4_pages", C.c_void_p), ("v4_pages", C.c_void_p), ("n_pages4", C.c_int64), ("page_table4", C.c_void_p),
+    _fields_ = [("kv4_pages", C.c_void_p), ("n_pages4", C.c_int64), ("page_table4", C.c_void_p),
                 ("max_query_tokens", C.c_int32), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
 
 
-Q4_UNIT_ROWS, Q4_UNIT_BYTES = 16, 1152
+Q4_UNIT_ROWS, Q4_UNIT_BYTES = 16, 2304
 
 _lib = None
 _bind = None
@@ -443,7 +443,7 @@ class Store:
         if ws_bytes == 0:
             raise KveError("kvE_q4_workspace_bytes", -2, "unsupported geometry")
         page_bytes = self.C // Q4_UNIT_ROWS * Q4_UNIT_BYTES
-        k4, v4 = (torch.zeros((n_pages, page_bytes), dtype=torch.uint8, device=self.device) for _ in range(2))
+        kv4 = torch.zeros((n_pages, page_bytes), dtype=torch.uint8, device=self.device)
         if page_perm is None:
             pt = np.arange(n_pages, dtype=np.int32)
         elif isinstance(page_perm, str) and page_perm == "random":
@@ -452,10 +452,10 @@ class Store:
             pt = np.asarray(page_perm, np.int32)
         table = torch.from_numpy(pt.reshape(self.n_layers, self.S, self.max_chunks).copy()).to(self.device)
         workspace = torch.zeros((ws_bytes + 256,), dtype=torch.uint8, device=self.device)
-        buf = kvE_q4_buffers(k4_pages=k4.data_ptr(), v4_pages=v4.data_ptr(), n_pages4=n_pages, page_table4=table.data_ptr(),
+        buf = kvE_q4_buffers(kv4_pages=kv4.data_ptr(), n_pages4=n_pages, page_table4=table.data_ptr(),
                              max_query_tokens=int(max_query_tokens), workspace=(workspace.data_ptr() + 255) // 256 * 256, workspace_bytes=ws_bytes)
         _check("kvE_attach_q4", self.lib.kvE_attach_q4(self.handle, C.byref(buf)), self.handle)
-        self.k4_pages, self.v4_pages, self.page_table4, self.q4_workspace = k4, v4, table, workspace
+        self.kv4_pages, self.page_table4, self.q4_workspace = kv4, table, workspace
 
     def pack_chunks(self, layer, chunk_begin, chunk_end, stream=None):
         """chunks outside the window to 4 bits"""

@@ -991,7 +991,7 @@ int check_q4(const kvE_config* c, int max_query_tokens) {
   return KVE_OK;
 }
 Q4Pages q4_pages(const kvE_store* st, int layer) {
-  return Q4Pages{static_cast<uint8_t*>(st->q4.k4_pages), static_cast<uint8_t*>(st->q4.v4_pages), st->q4.n_pages4,
+  return Q4Pages{static_cast<uint8_t*>(st->q4.kv4_pages), st->q4.n_pages4,
                  st->q4.page_table4 + (size_t)layer * st->S * st->max_chunks};
 }
 
@@ -1040,12 +1040,11 @@ size_t kvE_q4_workspace_bytes(const kvE_config* cfg, int max_query_tokens) {
 }
 
 int kvE_attach_q4(kvE_store* st, const kvE_q4_buffers* buf) {
-  if (!st || !buf || !buf->k4_pages || !buf->v4_pages || !buf->page_table4 || !buf->workspace || buf->n_pages4 <= 0) return KVE_ERR_ARG;
+  if (!st || !buf || !buf->kv4_pages || !buf->page_table4 || !buf->workspace || buf->n_pages4 <= 0) return KVE_ERR_ARG;
   if (wrong_device(st)) return KVE_ERR_STATE;
   const int rc = check_q4(&st->cfg, buf->max_query_tokens);
   if (rc != KVE_OK) return rc;
-  for (const void* p : {buf->k4_pages, buf->v4_pages})
-    if (reinterpret_cast<uintptr_t>(p) % 16 != 0) return KVE_ERR_ARG;
+  if (reinterpret_cast<uintptr_t>(buf->kv4_pages) % 16 != 0) return KVE_ERR_ARG;
   if (reinterpret_cast<uintptr_t>(buf->workspace) % ALIGN != 0) return KVE_ERR_ARG;
   const Q4Carve k = q4_carve(st->cfg, buf->max_query_tokens);
   if (buf->workspace_bytes < k.total) return KVE_ERR_CAPACITY;

@@ -88,11 +88,11 @@ cudaError_t launch_append_rope(const LayerView& v, const RopeCall& call, bool ne
 
 // the cache in 4 bits (layout: q4.cuh)
 struct Q4Pages {
-  uint8_t *k, *v;             // [n_pages][C / 16][Q4_UNIT_BYTES]
+  uint8_t* kv;                // [n_pages][C / 16][keys' unit, values' unit]
   long long n_pages;
   const int32_t* table;       // [S][max_chunks], this layer's
 };
-constexpr int Q4_UNIT_ROWS = 16, Q4_UNIT_BYTES = 1152;
+constexpr int Q4_UNIT_ROWS = 16, Q4_UNIT_BYTES = 1152, Q4_PAIR_BYTES = 2 * Q4_UNIT_BYTES;
 cudaError_t launch_pack(const LayerView& v, const Q4Pages& p, int t0, int t1, int n_packed, cudaStream_t st);
 cudaError_t launch_unpack(const LayerView& v, const Q4Pages& p, int t0, int t1, void* k_out, void* v_out, cudaStream_t st);
 // attention of T query tokens on G query heads a KV head.  Query rows go in `groups` of `cols`, one CTA each; every sequence is cut into parts_per_seq equal

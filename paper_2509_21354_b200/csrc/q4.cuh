@@ -4,7 +4,7 @@
 // s = bf16((largest - low) / 15) and a code c of 4 bits for every number x: the count of borders low + (k + 1/2) s, k = 0..14, below x
 // (on a border: the lower code).  It stands for low + c s.
 //
-// Pages are made of units of 16 rows, 1152 bytes: 1024 of codes in the order in which a warp's lanes feed them to m16n8k16 MMAs, then
+// Pages are made of units of 16 rows, 1152 bytes of keys and 1152 of values behind them (so that one copy fetches both): 1024 of codes in the order in which a warp's lanes feed them to m16n8k16 MMAs, then
 // [16 rows][2 groups] pairs (s, low) of bf16.  A 32-bit word holds eight codes as four pairs: pair e in the bits 4 e .. 4 e + 3 of both
 // halves.  As the bits of an fp16 number a code c by itself is c 2^-24, and c << 4 is c 2^-20 (numbers without a leading one, which the tensor
 // cores take as exactly as others): two masks and a shift by 8 make four operand registers of a word.

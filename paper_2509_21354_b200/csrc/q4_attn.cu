@@ -29,8 +29,8 @@
 
 namespace kve {
 
-constexpr int QA_TILE_BYTES = 4 * Q4_UNIT_BYTES;             // two units of keys, two of values
-constexpr int QA_V_OFF = 2 * Q4_UNIT_BYTES;                  // values behind the keys
+constexpr int QA_TILE_BYTES = 2 * Q4_PAIR_BYTES;             // two units of keys and values
+constexpr int QA_V_OFF = 2 * Q4_UNIT_BYTES;                  // bf16 rows: values behind the keys
 constexpr int QA_ROWS4 = 2 * Q4_UNIT_ROWS, QA_ROWS16 = 8;    // rows of a tile of either kind
 static_assert(QA_ROWS16 * ROW_BYTES <= QA_V_OFF, "eight bf16 rows fit a stage");
 constexpr float QA_SLACK = 8.f;                              // by how much (log2) a logit may pass the softmax reference
@@ -311,11 +311,17 @@ __global__ void __launch_bounds__(QaShape<NT>::WARPS * 32, 1) kve_decode_attn_q4
         if (e.z != 0) {
           unsigned char* dst = smem + (w * STAGES + stage) * QA_TILE_BYTES;
           const bool in4 = e.z > 0;
-          const uint32_t row_bytes = in4 ? Q4_UNIT_BYTES / Q4_UNIT_ROWS : ROW_BYTES, bytes = (uint32_t)abs(e.z) * row_bytes;
-          const long long at = ((long long)e.x * v.C + e.y) * row_bytes;
-          mbar_arrive_expect_tx(&my_full[stage], 2 * bytes);      // release: whoever sees the phase sees the description
-          bulk_g2s(dst, (in4 ? a.p.k : reinterpret_cast<const uint8_t*>(v.k_pages)) + at, bytes, &my_full[stage]);
-          bulk_g2s(dst + QA_V_OFF, (in4 ? a.p.v : reinterpret_cast<const uint8_t*>(v.v_pages)) + at, bytes, &my_full[stage]);
+          const long long row = (long long)e.x * v.C + e.y;
+          if (in4) {
+            const uint32_t bytes = (uint32_t)e.z * (Q4_PAIR_BYTES / Q4_UNIT_ROWS);
+            mbar_arrive_expect_tx(&my_full[stage], bytes);      // release: whoever sees the phase sees the description
+            bulk_g2s(dst, a.p.kv + row * (Q4_PAIR_BYTES / Q4_UNIT_ROWS), bytes, &my_full[stage]);
+          } else {
+            const uint32_t bytes = (uint32_t)-e.z * ROW_BYTES;
+            mbar_arrive_expect_tx(&my_full[stage], 2 * bytes);
+            bulk_g2s(dst, v.k_pages + row * D, bytes, &my_full[stage]);
+            bulk_g2s(dst + QA_V_OFF, v.v_pages + row * D, bytes, &my_full[stage]);
+          }
         } else {
           mbar_arrive(&my_full[stage]);
         }
@@ -372,12 +378,13 @@ __global__ void __launch_bounds__(QaShape<NT>::WARPS * 32, 1) kve_decode_attn_q4
     // per column: the softmax's reference (0 until there is one), and what a logit may exceed it by (-inf until there is one)
     float ref[NT][2], over_by[NT][2];
     float F[2];      // weight factor of either half: the largest p s so far times F lies in [2^6, 2^7); a scale with s F > 2^7 asks for another
+      // (2^64 at most, and to begin with: sums of bf16 rows times F stay finite below |v| = 2^60)
     // a fresh state, and the query rows in slot `slot`
     auto start = [&](int slot) {
       Qh = reinterpret_cast<const uint16_t*>(smem + Shape::OFF_QH) + slot * COLS * D;
       Qb = reinterpret_cast<const uint16_t*>(smem + Shape::OFF_Q) + slot * COLS * D;
       const float* q_undo = reinterpret_cast<const float*>(smem + Shape::OFF_UNDO) + slot * COLS;
-      F[0] = F[1] = 0x1p120f;
+      F[0] = F[1] = 0x1p64f;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         float sum[2] = {0.f, 0.f};
@@ -445,7 +452,7 @@ __global__ void __launch_bounds__(QaShape<NT>::WARPS * 32, 1) kve_decode_attn_q4
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const float largest = fmaxf(64.f / F[h] * most, warp_max(h ? s1 : s0));
-          const int e = min(max((int)(__float_as_uint(largest) >> 23) - 127, -110), 126);
+          const int e = min(max((int)(__float_as_uint(largest) >> 23) - 127, -58), 126);
           const float to = __uint_as_float((uint32_t)(127 + 6 - e) << 23), f = to / F[h];
           F[h] = to;
 #pragma unroll
@@ -479,8 +486,8 @@ __global__ void __launch_bounds__(QaShape<NT>::WARPS * 32, 1) kve_decode_attn_q4
         uint4 ka[UNITS], kc[UNITS];
 #pragma unroll
         for (int u = 0; u < UNITS; ++u) {
-          ka[u] = *reinterpret_cast<const uint4*>(base + u * Q4_UNIT_BYTES + lane * 16);
-          kc[u] = *reinterpret_cast<const uint4*>(base + u * Q4_UNIT_BYTES + 512 + lane * 16);
+          ka[u] = *reinterpret_cast<const uint4*>(base + u * Q4_PAIR_BYTES + lane * 16);
+          kc[u] = *reinterpret_cast<const uint4*>(base + u * Q4_PAIR_BYTES + 512 + lane * 16);
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -505,7 +512,7 @@ __global__ void __launch_bounds__(QaShape<NT>::WARPS * 32, 1) kve_decode_attn_q4
         // x = low + s c: the sum over a group is s (what the MMAs give) + low (sum of q)
 #pragma unroll
         for (int u = 0; u < UNITS; ++u) {
-          const uint2 ha = *reinterpret_cast<const uint2*>(base + u * Q4_UNIT_BYTES + Q4_CODE_BYTES + g8 * 8), hc = *reinterpret_cast<const uint2*>(base + u * Q4_UNIT_BYTES + Q4_CODE_BYTES + 64 + g8 * 8);
+          const uint2 ha = *reinterpret_cast<const uint2*>(base + u * Q4_PAIR_BYTES + Q4_CODE_BYTES + g8 * 8), hc = *reinterpret_cast<const uint2*>(base + u * Q4_PAIR_BYTES + Q4_CODE_BYTES + 64 + g8 * 8);
           const float sa0 = bf16lo(ha.x), sa1 = bf16lo(ha.y), sc0 = bf16lo(hc.x), sc1 = bf16lo(hc.y);
           const float la0 = bf16hi(ha.x), la1 = bf16hi(ha.y), lc0 = bf16hi(hc.x), lc1 = bf16hi(hc.y);
 #pragma unroll
@@ -516,8 +523,8 @@ __global__ void __launch_bounds__(QaShape<NT>::WARPS * 32, 1) kve_decode_attn_q4
               x[nt][4 * u + c] = fmaf(fmaf(y[0][c], sa0, y[1][c] * sa1), undo[nt][c], fmaf(la0, qsum[nt][0][c], fmaf(la1, qsum[nt][1][c], -ref[nt][c])));
               x[nt][4 * u + 2 + c] = fmaf(fmaf(y[0][2 + c], sc0, y[1][2 + c] * sc1), undo[nt][c], fmaf(lc0, qsum[nt][0][c], fmaf(lc1, qsum[nt][1][c], -ref[nt][c])));
             }
-          va[u] = *reinterpret_cast<const uint2*>(base + QA_V_OFF + u * Q4_UNIT_BYTES + Q4_CODE_BYTES + g8 * 8);
-          vc[u] = *reinterpret_cast<const uint2*>(base + QA_V_OFF + u * Q4_UNIT_BYTES + Q4_CODE_BYTES + 64 + g8 * 8);
+          va[u] = *reinterpret_cast<const uint2*>(base + u * Q4_PAIR_BYTES + Q4_UNIT_BYTES + Q4_CODE_BYTES + g8 * 8);
+          vc[u] = *reinterpret_cast<const uint2*>(base + u * Q4_PAIR_BYTES + Q4_UNIT_BYTES + Q4_CODE_BYTES + 64 + g8 * 8);
         }
       }
       float s0 = 0.f, s1 = 0.f;
@@ -535,7 +542,7 @@ __global__ void __launch_bounds__(QaShape<NT>::WARPS * 32, 1) kve_decode_attn_q4
         for (int u = 0; u < UNITS; ++u) {
           const uint32_t ga = h ? va[u].y : va[u].x, gc = h ? vc[u].y : vc[u].x;
           const float f_a = bf16lo(ga) * F[h], f_c = bf16lo(gc) * F[h], l_a = bf16hi(ga), l_c = bf16hi(gc);
-          vw[u] = *reinterpret_cast<const uint4*>(base + QA_V_OFF + u * Q4_UNIT_BYTES + h * 512 + lane * 16);
+          vw[u] = *reinterpret_cast<const uint4*>(base + u * Q4_PAIR_BYTES + Q4_UNIT_BYTES + h * 512 + lane * 16);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
             const float* p = &x[nt][4 * u];
@@ -566,7 +573,7 @@ __global__ void __launch_bounds__(QaShape<NT>::WARPS * 32, 1) kve_decode_attn_q4
 
     // a tile of `rows` <= 8 bf16 rows, the first at position pos
     auto bf16_rows = [&](int rows, int pos, const unsigned char* base) {
-      float x[NT][4];
+      float x[NT][2];
       {
         float d[NT][2][4];
         const uint4* kr = reinterpret_cast<const uint4*>(base + g8 * ROW_BYTES) + t4;
@@ -585,29 +592,29 @@ __global__ void __launch_bounds__(QaShape<NT>::WARPS * 32, 1) kve_decode_attn_q4
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            const bool seen = g8 < rows && pos + g8 <= last_pos(nt, c);
-            x[nt][c] = seen ? fmaf(d[nt][0][c] + d[nt][1][c], sl2, -ref[nt][c]) : -INFINITY;
-            x[nt][2 + c] = -INFINITY;
-          }
+          for (int c = 0; c < 2; ++c) x[nt][c] = fmaf(d[nt][0][c] + d[nt][1][c], sl2, -ref[nt][c]);
+        if (rows < QA_ROWS16 || a.causal) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+              if (g8 >= rows || pos + g8 > last_pos(nt, c)) x[nt][c] = -INFINITY;
+        }
       }
       uint4 e[2], o[2];      // this lane's numbers of the rows 2 t4 and 2 t4 + 1
-      float largest[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         e[h] = *reinterpret_cast<const uint4*>(base + QA_V_OFF + 2 * t4 * ROW_BYTES + h * 128 + g8 * 16);
         o[h] = *reinterpret_cast<const uint4*>(base + QA_V_OFF + (2 * t4 + 1) * ROW_BYTES + h * 128 + g8 * 16);
-        if (2 * t4 >= rows) e[h] = make_uint4(0u, 0u, 0u, 0u);      // what an earlier tile left there may be anything
-        if (2 * t4 + 1 >= rows) o[h] = make_uint4(0u, 0u, 0u, 0u);
-        auto larger = [](uint32_t p, uint32_t q) {
-          uint32_t d;
-          asm("max.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(p & 0x7fff7fffu), "r"(q & 0x7fff7fffu));
-          return d;
-        };
-        const uint32_t most = larger(larger(larger(e[h].x, e[h].y), larger(e[h].z, e[h].w)), larger(larger(o[h].x, o[h].y), larger(o[h].z, o[h].w)));
-        largest[h] = fmaxf(bf16lo(most), bf16hi(most)) * 0.125f;      // (as a scale: codes reach 8 from the middle)
       }
-      weigh(x, largest[0], largest[1]);
+      if (rows < QA_ROWS16) {      // what an earlier tile left there may be anything
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          if (2 * t4 >= rows) e[h] = make_uint4(0u, 0u, 0u, 0u);
+          if (2 * t4 + 1 >= rows) o[h] = make_uint4(0u, 0u, 0u, 0u);
+        }
+      }
+      weigh(x, 0.f, 0.f);
       // both planes of the weights in one MMA: rows 0-7 of its contraction have the first, rows 8-15, the same rows again, the second
       uint32_t b[NT][2];
 #pragma unroll

@@ -95,7 +95,7 @@ __global__ void __launch_bounds__(PK_WARPS * 32) kve_pack_kernel(LayerView v, Q4
   }
   const int half = lane >> 4, l16 = lane & 15;
   const uint4* src = reinterpret_cast<const uint4*>((is_v ? v.v_pages : v.k_pages) + (page * v.C + unit * Q4_UNIT_ROWS) * D) + lane;
-  uint8_t* dst = (is_v ? p.v : p.k) + (page4 * per_chunk + unit) * Q4_UNIT_BYTES;
+  uint8_t* dst = p.kv + (page4 * per_chunk + unit) * Q4_PAIR_BYTES + (is_v ? Q4_UNIT_BYTES : 0);
   uint4 row[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) row[i] = __ldcs(src + i * 32);      // rows 2 i + half
@@ -168,7 +168,7 @@ __global__ void __launch_bounds__(PK_WARPS * 32) kve_unpack_kernel(LayerView v, 
     return;
   }
   const int half = lane >> 4, l16 = lane & 15;
-  const uint8_t* src = (is_v ? p.v : p.k) + (page4 * per_chunk + unit) * Q4_UNIT_BYTES;
+  const uint8_t* src = p.kv + (page4 * per_chunk + unit) * Q4_PAIR_BYTES + (is_v ? Q4_UNIT_BYTES : 0);
   uint4* dst = reinterpret_cast<uint4*>((is_v ? v_out : k_out) + ((long long)x * v.C + unit * Q4_UNIT_ROWS) * D) + lane;
   uint32_t* cw = codes[warp];
   // keys: lane (row, t) has the words j = 0..3, numbers 32 j + 8 t .. + 7: word 4 j + t of the row;

@@ -8,6 +8,8 @@
 // HBM-bound: (Hq + 2 Hkv) rows of 256 bytes a token are read and written once.  All heads of a token share its 64 angles, so a CTA
 // takes whole tokens: its first threads work out the angles while the first rows are on their way, the rest is one pass.  A thread holds
 // the 16 numbers of eight pairs of one row (two 16-byte pieces, 64 numbers apart or side by side), eight threads a row.
+#include <type_traits>
+
 #include "common.cuh"
 #include "kernels.h"
 
@@ -78,9 +80,21 @@ __global__ void __launch_bounds__(RP_THREADS, RP_CTAS) kve_append_rope_kernel(La
     const int w = tid >> 5, e = tid & 7;
     double turns = 0.0;
     int axis = 0;
+    auto pick = [&](auto first) {
 #pragma unroll
-    for (int j = 0; j < 64; ++j)
-      if (8 * w + e == j) { turns = a.turns[j]; axis = a.axis[j]; }
+      for (int j = 0; j < 8; ++j)
+        if (e == j) { turns = a.turns[decltype(first)::value + j]; axis = a.axis[decltype(first)::value + j]; }
+    };
+    switch (w) {
+      case 0: pick(std::integral_constant<int, 0>()); break;
+      case 1: pick(std::integral_constant<int, 8>()); break;
+      case 2: pick(std::integral_constant<int, 16>()); break;
+      case 3: pick(std::integral_constant<int, 24>()); break;
+      case 4: pick(std::integral_constant<int, 32>()); break;
+      case 5: pick(std::integral_constant<int, 40>()); break;
+      case 6: pick(std::integral_constant<int, 48>()); break;
+      default: pick(std::integral_constant<int, 56>()); break;
+    }
     for (int tok = (tid & 31) >> 3; tok < n_tok; tok += 4) {
       const int t = tok0 + tok;
       int pos;

@@ -37,8 +37,7 @@ class Case:
         # whatever is read although it should not be shows
         st.k_pages.fill_(float("nan"))
         st.v_pages.fill_(float("nan"))
-        st.k4_pages.fill_(0xFF)
-        st.v4_pages.fill_(0xFF)
+        st.kv4_pages.fill_(0xFF)
         self.stale = max(0, n - W) // C_
         self.packed = self.stale if packed is None else packed
         self.K = normal((st.S, n, 128), seed + 2) if K is None else K
@@ -331,7 +330,7 @@ def test_layers_are_apart():
     case.check(dense=True)
     q = normal((1, 1, 2, 128), 1)
     assert (st.decode_attn_q4(0, q) == 0).all()
-    assert (st.k4_pages[st.page_table4[0].flatten().long()] == 0xFF).all()
+    assert (st.kv4_pages[st.page_table4[0].flatten().long()] == 0xFF).all()
 
 
 def test_a_decode_loop_from_a_graph():
@@ -492,10 +491,10 @@ def test_refusals():
     with pytest.raises(AssertionError):
         case.st.decode_attn_q4(0, q[:, :, :1])
     # attach: buffers are checked before they are taken
-    buf = lambda **kw: C.byref(b.kvE_q4_buffers(**{**dict(k4_pages=st.k4_pages.data_ptr(), v4_pages=st.v4_pages.data_ptr(), n_pages4=4, page_table4=st.page_table4.data_ptr(),
+    buf = lambda **kw: C.byref(b.kvE_q4_buffers(**{**dict(kv4_pages=st.kv4_pages.data_ptr(), n_pages4=4, page_table4=st.page_table4.data_ptr(),
                                                         max_query_tokens=1, workspace=(st.q4_workspace.data_ptr() + 255) // 256 * 256, workspace_bytes=st.q4_workspace.numel() - 256), **kw}))
     attach = lambda **kw: lib.kvE_attach_q4(h, buf(**kw))
-    assert attach(k4_pages=None) == attach(v4_pages=st.v4_pages.data_ptr() + 4) == attach(n_pages4=0) == attach(page_table4=None) == attach(workspace=None) == -1
+    assert attach(kv4_pages=None) == attach(kv4_pages=st.kv4_pages.data_ptr() + 4) == attach(n_pages4=0) == attach(page_table4=None) == attach(workspace=None) == -1
     assert attach(workspace_bytes=10) == -3 and attach(max_query_tokens=100) == -2 and attach(max_query_tokens=0) == -1
     assert st.packed_chunks(0) == 1
 
@@ -503,9 +502,9 @@ def test_refusals():
 def test_attaching_again_starts_empty():
     case = Case(n=300)
     assert case.st.packed_chunks(0) == 3
-    old = case.st.k4_pages
+    old = case.st.kv4_pages
     case.st.attach_q4()
-    assert case.st.packed_chunks(0) == 0 and case.st.k4_pages.data_ptr() != old.data_ptr()
+    assert case.st.packed_chunks(0) == 0 and case.st.kv4_pages.data_ptr() != old.data_ptr()
     case.packed = 0
     case.check(dense=True)
 

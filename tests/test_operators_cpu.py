@@ -17,7 +17,7 @@ def config(**kw):
 def test_struct_layouts():
     assert C.sizeof(b.kvE_rope) == 4 + 4 + 64 + 64 * 8
     assert C.sizeof(b.kvE_rows) == 4 * 8
-    assert C.sizeof(b.kvE_q4_buffers) == 7 * 8
+    assert C.sizeof(b.kvE_q4_buffers) == 6 * 8
 
 
 def test_q4_workspace_and_geometry():
