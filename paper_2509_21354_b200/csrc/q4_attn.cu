@@ -10,6 +10,8 @@
 //    p s per group of 64 dims).  q enters as fp16 as well, times a power of two that puts its largest number at 2^14: exact but for numbers 2^25 below that.
 //  * both products are m16n8k16 MMAs with the cache on the M side (keys: 16 rows; values, transposed: 16 dims) and the queries in the
 //    eight columns.  The logits' accumulator becomes the weights' operand through movmatrix, in registers.
+//  * up to four query rows: the eight columns are the four rows twice, once for either group of 64 dims (q is zero in the other half; the weights have the
+//    group's scale), so that a lane has to do with one group only: half of the scales, weights and conversions (see DUO).
 //  * the weights p s F of packed rows are fp16: 11 bits, whose rounding (2^-12 a row) stays far below the result's own (2^-9).  F, a power of two per
 //    warp and group, follows the largest p s so that they neither overflow nor run out of bits.  bf16 rows take their weights as two bf16 planes.
 //  * a tile's products with the values are summed from zero and added to the accumulator by ordinary additions: the tensor core cuts off what lies below
@@ -51,15 +53,15 @@ struct Q4AttnArgs {
   int32_t* counters;    // [S][groups], zero between launches
 };
 
-template <int NT> struct QaShape {
-  static constexpr int COLS = 8 * NT;                        // query rows of a CTA
+template <int NT, bool DUO> struct QaShape {
+  static constexpr int MCOLS = 8 * NT, COLS = DUO ? 4 : MCOLS;      // columns of the MMAs; query rows of a CTA
   static constexpr int CW = NT == 1 ? 12 : 8;                // consumer warps
   static constexpr int PRODUCERS = 2, PLANNER = CW + PRODUCERS, MERGER = PLANNER + 1, WARPS = MERGER + 1;
   static constexpr int STAGES = 3;                           // per consumer
   static constexpr int OFF_STATE = CW * STAGES * QA_TILE_BYTES;                          // [consumers][query rows][132]: behind the ring
   static constexpr int OFF_Q = OFF_STATE + CW * COLS * ATTN_PARTIAL_FLOATS * 4;          // [2][query rows][128] bf16; the same as fp16; what undoes their powers of two: [2][query rows]
   static constexpr int OFF_QH = OFF_Q + 2 * COLS * ROW_BYTES;
-  static constexpr int OFF_UNDO = OFF_QH + 2 * COLS * ROW_BYTES;
+  static constexpr int OFF_UNDO = OFF_QH + 2 * MCOLS * ROW_BYTES;
   static constexpr int OFF_INFO = OFF_UNDO + 2 * COLS * 4;   // [consumers][stages] int4: the tile's entry of the table
   static constexpr int OFF_PLAN = OFF_INFO + CW * STAGES * 16;      // [QA_PLAN] int4: tiles looked up
   static constexpr int OFF_BAR = OFF_PLAN + QA_PLAN * 16;
@@ -119,11 +121,13 @@ __device__ __forceinline__ void write_row(const Q4AttnArgs& a, int s, int rr, fl
 __device__ __forceinline__ uint32_t qa_begin(uint32_t c, uint32_t I, uint32_t P) { return (c * I) / P; }
 __device__ __forceinline__ uint32_t qa_owner(uint32_t x, uint32_t I, uint32_t P) { return ((x + 1u) * P - 1u) / I; }
 
-// NT: column tiles of eight query rows
-template <int NT>
-__global__ void __launch_bounds__(QaShape<NT>::WARPS * 32, 1) kve_decode_attn_q4_kernel(Q4AttnArgs a) {
-  using Shape = QaShape<NT>;
-  constexpr int STAGES = Shape::STAGES, CW = Shape::CW, WARPS = Shape::WARPS, COLS = Shape::COLS;
+// NT: column tiles of eight query rows.  DUO (NT == 1): up to four query rows; columns 4 to 7 are columns 0 to 3 again, where the MMAs with packed rows have group 0
+// in the columns below 4 and group 1 in those from 4 on
+template <int NT, bool DUO>
+__global__ void __launch_bounds__(QaShape<NT, DUO>::WARPS * 32, 1) kve_decode_attn_q4_kernel(Q4AttnArgs a) {
+  using Shape = QaShape<NT, DUO>;
+  constexpr int STAGES = Shape::STAGES, CW = Shape::CW, WARPS = Shape::WARPS, COLS = Shape::COLS, MCOLS = Shape::MCOLS;
+  constexpr int NG = DUO ? 1 : 2;      // groups that a lane has to do with
   extern __shared__ __align__(128) unsigned char smem[];
   const LayerView& v = a.v;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g8 = lane >> 2, t4 = lane & 3;
@@ -161,7 +165,7 @@ __global__ void __launch_bounds__(QaShape<NT>::WARPS * 32, 1) kve_decode_attn_q4
 
   // ---- a warp brings the query rows of sequence s into slot `slot`: bf16, and fp16 times a power of two ----
   auto fetch_queries = [&](int s, int slot) {
-    uint32_t* Qh = reinterpret_cast<uint32_t*>(smem + Shape::OFF_QH) + slot * COLS * 64;
+    uint32_t* Qh = reinterpret_cast<uint32_t*>(smem + Shape::OFF_QH) + slot * MCOLS * 64;
     uint4* Qb = reinterpret_cast<uint4*>(smem + Shape::OFF_Q) + slot * COLS * 16;
     float* q_undo = reinterpret_cast<float*>(smem + Shape::OFF_UNDO) + slot * COLS;
     const int b = (int)a.by_h.div((uint32_t)s), h = s - b * v.H, piece = lane & 15;
@@ -187,7 +191,13 @@ __global__ void __launch_bounds__(QaShape<NT>::WARPS * 32, 1) kve_decode_attn_q4
 #pragma unroll
       for (int e = 0; e < 4; ++e) {      // odd pairs meet codes that are 2^4 times as large
         const float f = e & 1 ? up * 0.0625f : up;
-        Qh[c * 64 + piece * 4 + e] = pack_f16x2(bf16lo(word[e]) * f, bf16hi(word[e]) * f);
+        const uint32_t w16 = pack_f16x2(bf16lo(word[e]) * f, bf16hi(word[e]) * f);
+        if constexpr (DUO) {
+          Qh[c * 64 + piece * 4 + e] = piece < 8 ? w16 : 0u;
+          Qh[(c + 4) * 64 + piece * 4 + e] = piece < 8 ? 0u : w16;
+        } else {
+          Qh[c * 64 + piece * 4 + e] = w16;
+        }
       }
       if (piece == 0) q_undo[c] = __uint_as_float((uint32_t)(127 - power) << 23);
     }
@@ -367,36 +377,38 @@ __global__ void __launch_bounds__(QaShape<NT>::WARPS * 32, 1) kve_decode_attn_q4
     const uint16_t *Qh = nullptr, *Qb = nullptr;      // its query rows, as fp16 and as bf16
     // column nt 8 + g8: the numbers 32 j + 8 t4 .. + 7, as fp16 (from shared memory every time)
     auto q_half = [&](int nt, int j) { return *reinterpret_cast<const uint4*>(Qh + (nt * 8 + g8) * D + 32 * j + 8 * t4); };
-    float undo[NT][2], qsum[NT][2][2];      // per column 2 t4, 2 t4 + 1: what takes q's power of two off a sum of codes (2^-24) and makes it a log2 logit; sums of q over the halves
+    float undo[NT][2], qsum[NT][NG][2];     // per column 2 t4, 2 t4 + 1: what takes q's power of two off a sum of codes (2^-24) and makes it a log2 logit; sums of q over the groups
     int n = 0;                              // tokens stored (read where it matters)
+    auto row_of = [&](int nt, int c) { return nt * 8 + (DUO ? c & 3 : c); };      // the query row of a column
     auto last_pos = [&](int nt, int x) {    // causal: the last position a column sees
-      return a.causal ? n - a.T + (int)a.by_g.div((uint32_t)min(row0 + nt * 8 + 2 * t4 + x, R - 1)) : 0x7fffffff;
+      return a.causal ? n - a.T + (int)a.by_g.div((uint32_t)min(row0 + row_of(nt, 2 * t4 + x), R - 1)) : 0x7fffffff;
     };
 
     float acc[NT][8][4];           // [m]: dims d = 64 (m / 4) + 8 g8 + 2 (m % 4) and d + 1, columns 2 t4 and 2 t4 + 1: (d, c), (d, c + 1), times F 2^-24; (d + 1, c), (d + 1, c + 1), times F 2^-20
-    float l[NT][2], zs[NT][2][2];  // this lane's rows' share, per column: sum of weights; of weights times what code 0 stands for
+    float l[NT][2], zs[NT][NG][2]; // this lane's rows' share, per column: sum of weights; of weights times what code 0 stands for
     // per column: the softmax's reference (0 until there is one), and what a logit may exceed it by (-inf until there is one)
     float ref[NT][2], over_by[NT][2];
-    float F[2];      // weight factor of either half: the largest p s so far times F lies in [2^6, 2^7); a scale with s F > 2^7 asks for another
+    float F[NG];     // weight factor of a group: the largest p s so far times F lies in [2^6, 2^7); a scale with s F > 2^7 asks for another
       // (2^64 at most, and to begin with: sums of bf16 rows times F stay finite below |v| = 2^60)
     // a fresh state, and the query rows in slot `slot`
     auto start = [&](int slot) {
-      Qh = reinterpret_cast<const uint16_t*>(smem + Shape::OFF_QH) + slot * COLS * D;
+      Qh = reinterpret_cast<const uint16_t*>(smem + Shape::OFF_QH) + slot * MCOLS * D;
       Qb = reinterpret_cast<const uint16_t*>(smem + Shape::OFF_Q) + slot * COLS * D;
       const float* q_undo = reinterpret_cast<const float*>(smem + Shape::OFF_UNDO) + slot * COLS;
-      F[0] = F[1] = 0x1p64f;
+#pragma unroll
+      for (int g = 0; g < NG; ++g) F[g] = 0x1p64f;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        float sum[2] = {0.f, 0.f};
+        float sum[NG] = {};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const uint4 w = q_half(nt, j);
           const float2 e0 = f16_pair(w.x), e1 = f16_pair(w.y), e2 = f16_pair(w.z), e3 = f16_pair(w.w);
-          sum[j >> 1] += (e0.x + e0.y) + (e2.x + e2.y) + 16.f * ((e1.x + e1.y) + (e3.x + e3.y));
+          sum[DUO ? 0 : j >> 1] += (e0.x + e0.y) + (e2.x + e2.y) + 16.f * ((e1.x + e1.y) + (e3.x + e3.y));
         }
-        const float off = q_undo[nt * 8 + g8] * sl2;
+        const float off = q_undo[row_of(nt, g8)] * sl2;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < NG; ++h) {
           float y = sum[h];
           y += __shfl_xor_sync(0xffffffffu, y, 1);
           y += __shfl_xor_sync(0xffffffffu, y, 2);      // of column g8, in its four lanes
@@ -406,8 +418,10 @@ __global__ void __launch_bounds__(QaShape<NT>::WARPS * 32, 1) kve_decode_attn_q4
         }
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          undo[nt][c] = q_undo[nt * 8 + 2 * t4 + c] * 0x1p12f * sl2 * 0x1p12f;
-          ref[nt][c] = 0.f; over_by[nt][c] = -INFINITY; l[nt][c] = 0.f; zs[nt][0][c] = zs[nt][1][c] = 0.f;
+          undo[nt][c] = q_undo[row_of(nt, 2 * t4 + c)] * 0x1p12f * sl2 * 0x1p12f;
+          ref[nt][c] = 0.f; over_by[nt][c] = -INFINITY; l[nt][c] = 0.f;
+#pragma unroll
+          for (int g = 0; g < NG; ++g) zs[nt][g][c] = 0.f;
         }
 #pragma unroll
         for (int m = 0; m < 8; ++m)
@@ -416,11 +430,13 @@ __global__ void __launch_bounds__(QaShape<NT>::WARPS * 32, 1) kve_decode_attn_q4
       }
     };
 
-    // Logits minus reference (log2 units; of each of this lane's rows: c, c + 1) to weights in place.  s0, s1: the largest scale of
-    // these rows in either half.  Raises reference and factors where it has to.
+    // Logits minus reference (log2 units; of each of this lane's rows: c, c + 1) to weights in place.  s: the largest scale of
+    // these rows in either group.  Raises reference and factors where it has to.
     auto weigh = [&](auto& x, float s0, float s1) {
       constexpr int N = (int)(sizeof(x[0]) / sizeof(float));
-      bool over = s0 * F[0] > 128.f || s1 * F[1] > 128.f;
+      bool over = false;
+#pragma unroll
+      for (int g = 0; g < NG; ++g) over |= (g ? s1 : s0) * F[g] > 128.f;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -444,23 +460,29 @@ __global__ void __launch_bounds__(QaShape<NT>::WARPS * 32, 1) kve_decode_attn_q4
             ref[nt][c] = to;
 #pragma unroll
             for (int i = c; i < N; i += 2) x[nt][i] -= up;
-            l[nt][c] *= f; zs[nt][0][c] *= f; zs[nt][1][c] *= f;
+            l[nt][c] *= f;
+#pragma unroll
+            for (int g = 0; g < NG; ++g) zs[nt][g][c] *= f;
 #pragma unroll
             for (int m = 0; m < 8; ++m) { acc[nt][m][c] *= f; acc[nt][m][2 + c] *= f; }
           }
         most = warp_max(most);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const float largest = fmaxf(64.f / F[h] * most, warp_max(h ? s1 : s0));
+        for (int g = 0; g < NG; ++g) {
+          float largest = g ? s1 : s0;      // of the group: DUO has the other one in the lanes t4 ^ 2
+#pragma unroll
+          for (int o = 16; o > 0; o >>= 1)
+            if (!DUO || o != 2) largest = fmaxf(largest, __shfl_xor_sync(0xffffffffu, largest, o));
+          largest = fmaxf(64.f / F[g] * most, largest);
           const int e = min(max((int)(__float_as_uint(largest) >> 23) - 127, -58), 126);
-          const float to = __uint_as_float((uint32_t)(127 + 6 - e) << 23), f = to / F[h];
-          F[h] = to;
+          const float to = __uint_as_float((uint32_t)(127 + 6 - e) << 23), f = to / F[g];
+          F[g] = to;
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int m = 0; m < 4; ++m)
+            for (int m = 0; m < (DUO ? 8 : 4); ++m)      // (DUO: what the lane holds of the other group's dims is nobody's)
 #pragma unroll
-              for (int y = 0; y < 4; ++y) acc[nt][4 * h + m][y] *= f;
+              for (int y = 0; y < 4; ++y) acc[nt][4 * g + m][y] *= f;
         }
       }
 #pragma unroll
@@ -480,9 +502,9 @@ __global__ void __launch_bounds__(QaShape<NT>::WARPS * 32, 1) kve_decode_attn_q4
     auto packed_rows = [&](auto units, const unsigned char* base) {
       constexpr int UNITS = decltype(units)::value;
       float x[NT][4 * UNITS];
-      uint2 va[UNITS], vc[UNITS];
+      uint32_t va[UNITS][NG], vc[UNITS][NG];      // scale and lowest number of the rows g8 and g8 + 8, values
       {
-        float d[UNITS][NT][2][4];
+        float d[UNITS][NT][2][4];      // two chains: the groups; DUO: even and odd words
         uint4 ka[UNITS], kc[UNITS];
 #pragma unroll
         for (int u = 0; u < UNITS; ++u) {
@@ -503,55 +525,78 @@ __global__ void __launch_bounds__(QaShape<NT>::WARPS * 32, 1) kve_decode_attn_q4
 #pragma unroll
             for (int u = 0; u < UNITS; ++u) {
               const uint32_t A0[4] = {pa[u][0], pc[u][0], pa[u][1], pc[u][1]}, A1[4] = {pa[u][2], pc[u][2], pa[u][3], pc[u][3]};
-              if ((j & 1) == 0) mma_f16_first(d[u][nt][j >> 1], A0, qw.x, qw.y);
-              else mma_f16_next(d[u][nt][j >> 1], A0, qw.x, qw.y);
-              mma_f16_next(d[u][nt][j >> 1], A1, qw.z, qw.w);
+              float(&to)[4] = d[u][nt][DUO ? j & 1 : j >> 1];
+              if (DUO ? j < 2 : (j & 1) == 0) mma_f16_first(to, A0, qw.x, qw.y);
+              else mma_f16_next(to, A0, qw.x, qw.y);
+              mma_f16_next(to, A1, qw.z, qw.w);
             }
           }
         }
         // x = low + s c: the sum over a group is s (what the MMAs give) + low (sum of q)
 #pragma unroll
         for (int u = 0; u < UNITS; ++u) {
-          const uint2 ha = *reinterpret_cast<const uint2*>(base + u * Q4_PAIR_BYTES + Q4_CODE_BYTES + g8 * 8), hc = *reinterpret_cast<const uint2*>(base + u * Q4_PAIR_BYTES + Q4_CODE_BYTES + 64 + g8 * 8);
-          const float sa0 = bf16lo(ha.x), sa1 = bf16lo(ha.y), sc0 = bf16lo(hc.x), sc1 = bf16lo(hc.y);
-          const float la0 = bf16hi(ha.x), la1 = bf16hi(ha.y), lc0 = bf16hi(hc.x), lc1 = bf16hi(hc.y);
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
+          const unsigned char* kh = base + u * Q4_PAIR_BYTES + Q4_CODE_BYTES + g8 * 8;
+          const unsigned char* vh = kh + Q4_UNIT_BYTES;
+          if constexpr (DUO) {
+            // a lane has the sum of its own group; the other group's is in the lane t4 ^ 2
+            const int of = (t4 >> 1) * 4;
+            const uint32_t ha = *reinterpret_cast<const uint32_t*>(kh + of), hc = *reinterpret_cast<const uint32_t*>(kh + 64 + of);
+            const float sa = bf16lo(ha), sc = bf16lo(hc), la = bf16hi(ha), lc = bf16hi(hc);
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-              const float(&y)[2][4] = d[u][nt];
-              x[nt][4 * u + c] = fmaf(fmaf(y[0][c], sa0, y[1][c] * sa1), undo[nt][c], fmaf(la0, qsum[nt][0][c], fmaf(la1, qsum[nt][1][c], -ref[nt][c])));
-              x[nt][4 * u + 2 + c] = fmaf(fmaf(y[0][2 + c], sc0, y[1][2 + c] * sc1), undo[nt][c], fmaf(lc0, qsum[nt][0][c], fmaf(lc1, qsum[nt][1][c], -ref[nt][c])));
+              const float(&y)[2][4] = d[u][0];
+              const float half_ref = -0.5f * ref[0][c];
+              const float p = fmaf((y[0][c] + y[1][c]) * sa, undo[0][c], fmaf(la, qsum[0][0][c], half_ref));
+              const float q = fmaf((y[0][2 + c] + y[1][2 + c]) * sc, undo[0][c], fmaf(lc, qsum[0][0][c], half_ref));
+              x[0][4 * u + c] = p + __shfl_xor_sync(0xffffffffu, p, 2);
+              x[0][4 * u + 2 + c] = q + __shfl_xor_sync(0xffffffffu, q, 2);
             }
-          va[u] = *reinterpret_cast<const uint2*>(base + u * Q4_PAIR_BYTES + Q4_UNIT_BYTES + Q4_CODE_BYTES + g8 * 8);
-          vc[u] = *reinterpret_cast<const uint2*>(base + u * Q4_PAIR_BYTES + Q4_UNIT_BYTES + Q4_CODE_BYTES + 64 + g8 * 8);
+            va[u][0] = *reinterpret_cast<const uint32_t*>(vh + of);
+            vc[u][0] = *reinterpret_cast<const uint32_t*>(vh + 64 + of);
+          } else {
+            const uint2 ha = *reinterpret_cast<const uint2*>(kh), hc = *reinterpret_cast<const uint2*>(kh + 64), wa = *reinterpret_cast<const uint2*>(vh), wc = *reinterpret_cast<const uint2*>(vh + 64);
+            const float sa0 = bf16lo(ha.x), sa1 = bf16lo(ha.y), sc0 = bf16lo(hc.x), sc1 = bf16lo(hc.y);
+            const float la0 = bf16hi(ha.x), la1 = bf16hi(ha.y), lc0 = bf16hi(hc.x), lc1 = bf16hi(hc.y);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int c = 0; c < 2; ++c) {
+                const float(&y)[2][4] = d[u][nt];
+                x[nt][4 * u + c] = fmaf(fmaf(y[0][c], sa0, y[1][c] * sa1), undo[nt][c], fmaf(la0, qsum[nt][0][c], fmaf(la1, qsum[nt][NG - 1][c], -ref[nt][c])));
+                x[nt][4 * u + 2 + c] = fmaf(fmaf(y[0][2 + c], sc0, y[1][2 + c] * sc1), undo[nt][c], fmaf(lc0, qsum[nt][0][c], fmaf(lc1, qsum[nt][NG - 1][c], -ref[nt][c])));
+              }
+            va[u][0] = wa.x; va[u][NG - 1] = wa.y;
+            vc[u][0] = wc.x; vc[u][NG - 1] = wc.y;
+          }
         }
       }
-      float s0 = 0.f, s1 = 0.f;
+      float most[NG] = {};
 #pragma unroll
-      for (int u = 0; u < UNITS; ++u) {
-        s0 = fmaxf(s0, fmaxf(bf16lo(va[u].x), bf16lo(vc[u].x)));
-        s1 = fmaxf(s1, fmaxf(bf16lo(va[u].y), bf16lo(vc[u].y)));
-      }
-      weigh(x, s0, s1);
+      for (int u = 0; u < UNITS; ++u)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        uint32_t b[UNITS][NT][2];
-        uint4 vw[UNITS];
+        for (int g = 0; g < NG; ++g) most[g] = fmaxf(most[g], fmaxf(bf16lo(va[u][g]), bf16lo(vc[u][g])));
+      weigh(x, most[0], most[NG - 1]);
+      uint32_t b[NG][UNITS][NT][2];      // weights times scale: MMA operands
+#pragma unroll
+      for (int g = 0; g < NG; ++g)
 #pragma unroll
         for (int u = 0; u < UNITS; ++u) {
-          const uint32_t ga = h ? va[u].y : va[u].x, gc = h ? vc[u].y : vc[u].x;
-          const float f_a = bf16lo(ga) * F[h], f_c = bf16lo(gc) * F[h], l_a = bf16hi(ga), l_c = bf16hi(gc);
-          vw[u] = *reinterpret_cast<const uint4*>(base + u * Q4_PAIR_BYTES + Q4_UNIT_BYTES + h * 512 + lane * 16);
+          const float f_a = bf16lo(va[u][g]) * F[g], f_c = bf16lo(vc[u][g]) * F[g], l_a = bf16hi(va[u][g]), l_c = bf16hi(vc[u][g]);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
             const float* p = &x[nt][4 * u];
-            b[u][nt][0] = transpose_8x8(pack_f16x2(p[0] * f_a, p[1] * f_a));
-            b[u][nt][1] = transpose_8x8(pack_f16x2(p[2] * f_c, p[3] * f_c));
+            b[g][u][nt][0] = transpose_8x8(pack_f16x2(p[0] * f_a, p[1] * f_a));
+            b[g][u][nt][1] = transpose_8x8(pack_f16x2(p[2] * f_c, p[3] * f_c));
 #pragma unroll
-            for (int c = 0; c < 2; ++c) zs[nt][h][c] = fmaf(p[c], l_a, fmaf(p[2 + c], l_c, zs[nt][h][c]));
+            for (int c = 0; c < 2; ++c) zs[nt][g][c] = fmaf(p[c], l_a, fmaf(p[2 + c], l_c, zs[nt][g][c]));
           }
         }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int g = DUO ? 0 : h;
+        uint4 vw[UNITS];
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) vw[u] = *reinterpret_cast<const uint4*>(base + u * Q4_PAIR_BYTES + Q4_UNIT_BYTES + h * 512 + lane * 16);
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
           float d[NT][4];
@@ -561,8 +606,8 @@ __global__ void __launch_bounds__(QaShape<NT>::WARPS * 32, 1) kve_decode_attn_q4
             q4_spread(word_of(vw[u], m), A);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-              if (u == 0) mma_f16_first(d[nt], A, b[u][nt][0], b[u][nt][1]);
-              else mma_f16_next(d[nt], A, b[u][nt][0], b[u][nt][1]);
+              if (u == 0) mma_f16_first(d[nt], A, b[g][u][nt][0], b[g][u][nt][1]);
+              else mma_f16_next(d[nt], A, b[g][u][nt][0], b[g][u][nt][1]);
             }
           }
 #pragma unroll
@@ -583,7 +628,7 @@ __global__ void __launch_bounds__(QaShape<NT>::WARPS * 32, 1) kve_decode_attn_q4
           const uint32_t A0[4] = {kw.x, 0u, kw.y, 0u}, A1[4] = {kw.z, 0u, kw.w, 0u};
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
-            const uint4 qw = *reinterpret_cast<const uint4*>(Qb + (nt * 8 + g8) * D + 32 * jw + 8 * t4);
+            const uint4 qw = *reinterpret_cast<const uint4*>(Qb + row_of(nt, g8) * D + 32 * jw + 8 * t4);
             if ((jw & 1) == 0) mma_bf16_first(d[nt][jw >> 1], A0, qw.x, qw.y);
             else mma_bf16_next(d[nt][jw >> 1], A0, qw.x, qw.y);
             mma_bf16_next(d[nt][jw >> 1], A1, qw.z, qw.w);
@@ -626,7 +671,7 @@ __global__ void __launch_bounds__(QaShape<NT>::WARPS * 32, 1) kve_decode_attn_q4
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const uint32_t ew[4] = {e[h].x, e[h].y, e[h].z, e[h].w}, ow[4] = {o[h].x, o[h].y, o[h].z, o[h].w};
-        const float f01 = F[h] * 0x1p-24f, f23 = F[h] * 0x1p-20f;
+        const float f01 = F[DUO ? 0 : h] * 0x1p-24f, f23 = F[DUO ? 0 : h] * 0x1p-20f;
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
           const uint32_t a0 = __byte_perm(ew[m], ow[m], 0x5410), a1 = __byte_perm(ew[m], ow[m], 0x7632);
@@ -650,29 +695,29 @@ __global__ void __launch_bounds__(QaShape<NT>::WARPS * 32, 1) kve_decode_attn_q4
 #pragma unroll
           for (int o = 4; o <= 16; o <<= 1) {
             l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], o);
-            zs[nt][0][c] += __shfl_xor_sync(0xffffffffu, zs[nt][0][c], o);
-            zs[nt][1][c] += __shfl_xor_sync(0xffffffffu, zs[nt][1][c], o);
+#pragma unroll
+            for (int g = 0; g < NG; ++g) zs[nt][g][c] += __shfl_xor_sync(0xffffffffu, zs[nt][g][c], o);
           }
-      const float un[2] = {1.f / F[0], 1.f / F[1]};
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          float* st = states + (warp * COLS + nt * 8 + 2 * t4 + c) * ATTN_PARTIAL_FLOATS;
+          float* st = states + (warp * COLS + row_of(nt, 2 * t4 + c)) * ATTN_PARTIAL_FLOATS;
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const float zv = zs[nt][h][c];
-            float* o = st + 64 * h + 8 * g8;
+          for (int g = 0; g < NG; ++g) {
+            const float zv = zs[nt][g][c], un = 1.f / F[g];
+            float* o = st + 64 * (DUO ? t4 >> 1 : g) + 8 * g8;
             float y[8];
 #pragma unroll
             for (int m = 0; m < 4; ++m) {
-              y[2 * m] = fmaf(acc[nt][4 * h + m][c] * 0x1p24f, un[h], zv);
-              y[2 * m + 1] = fmaf(acc[nt][4 * h + m][2 + c] * 0x1p20f, un[h], zv);
+              const float even = DUO && t4 >= 2 ? acc[nt][4 + m][c] : acc[nt][4 * g + m][c], odd = DUO && t4 >= 2 ? acc[nt][4 + m][2 + c] : acc[nt][4 * g + m][2 + c];
+              y[2 * m] = fmaf(even * 0x1p24f, un, zv);
+              y[2 * m + 1] = fmaf(odd * 0x1p20f, un, zv);
             }
             *reinterpret_cast<float4*>(o) = make_float4(y[0], y[1], y[2], y[3]);
             *reinterpret_cast<float4*>(o + 4) = make_float4(y[4], y[5], y[6], y[7]);
           }
-          if (g8 == 0) { st[128] = over_by[nt][c] == -INFINITY ? -INFINITY : ref[nt][c]; st[129] = l[nt][c]; }
+          if (g8 == 0 && (!DUO || t4 < 2)) { st[128] = over_by[nt][c] == -INFINITY ? -INFINITY : ref[nt][c]; st[129] = l[nt][c]; }
         }
       __syncwarp();
     };
@@ -794,7 +839,7 @@ __global__ void __launch_bounds__(QaShape<NT>::WARPS * 32, 1) kve_decode_attn_q4
 }
 
 Q4AttnShape q4_attn_shape(int rows) {
-  const int cols = rows <= QaShape<1>::COLS ? QaShape<1>::COLS : QaShape<2>::COLS;
+  const int cols = rows <= QaShape<1, true>::COLS ? QaShape<1, true>::COLS : (rows <= QaShape<1, false>::COLS ? QaShape<1, false>::COLS : QaShape<2, false>::COLS);
   return {cols, (rows + cols - 1) / cols};
 }
 
@@ -813,9 +858,10 @@ cudaError_t launch_attn_q4(const LayerView& v, const Q4Pages& p, bool dense, int
     const cudaError_t e = smem_opt_in(opted, kernel, smem);
     return e != cudaSuccess ? e : launch_pdl(kernel, dim3((unsigned)(runs * shape.groups)), dim3((unsigned)warps * 32), (size_t)smem, st, a);
   };
-  static DeviceFlags f8, f16;
-  if (shape.cols == QaShape<1>::COLS) return launch(kve_decode_attn_q4_kernel<1>, f8, QaShape<1>::WARPS, QaShape<1>::SMEM);
-  return launch(kve_decode_attn_q4_kernel<2>, f16, QaShape<2>::WARPS, QaShape<2>::SMEM);
+  static DeviceFlags f4, f8, f16;
+  if (shape.cols == QaShape<1, true>::COLS) return launch(kve_decode_attn_q4_kernel<1, true>, f4, QaShape<1, true>::WARPS, QaShape<1, true>::SMEM);
+  if (shape.cols == QaShape<1, false>::COLS) return launch(kve_decode_attn_q4_kernel<1, false>, f8, QaShape<1, false>::WARPS, QaShape<1, false>::SMEM);
+  return launch(kve_decode_attn_q4_kernel<2, false>, f16, QaShape<2, false>::WARPS, QaShape<2, false>::SMEM);
 }
 
 }  // namespace kve
