@@ -10,7 +10,7 @@
  * Conventions for every entry point
  *   - returns KVE_OK (0) or a negative kvE_status; never throws, never aborts.
  *   - work is enqueued on the given CUDA stream (passed as void*, a cudaStream_t); the call does not
- *     wait for it.  kvE_poll_status and kvE_create are the only calls that synchronise.
+ *     wait for it.  kvE_poll_status, kvE_create and kvE_attach_q4 are the only calls that synchronise the device.
  *   - no entry point allocates or frees device memory.  Every device buffer is owned by the caller
  *     (allocate it with any allocator, e.g. PyTorch) and only borrowed; the handle owns host metadata.
  *   - argument and geometry errors are found on the host before any launch.  Device-side problems
@@ -356,7 +356,8 @@ int kvE_packed_chunks(const kvE_store* st, int layer, int* n_packed);
  * stays valid across triggers and further packing.  cfg.attend does not matter.
  *   causal != 0: the block's tokens are the newest of the cache and see it up to themselves; KVE_ERR_STATE if fewer rows than
  *   n_query_tokens lie behind the packed and listed chunks (a replay that comes to that sets KVE_ERR_CAPACITY).
- *   Products and sums in fp32, weights to 16 bits, one bf16 rounding of the result.  A row that sees nothing gives 0 and lse = -inf.
+ *   Sums in fp32, weights of packed rows to 11 bits (of bf16 rows to 16), one bf16 rounding of the result: values between 2^-60 and 2^60 in
+ *   magnitude, or 0.  (Scales below that lose bits; sums of larger bf16 rows beside them may overflow.)  A row that sees nothing gives 0 and lse = -inf.
  *   q, out: DEVICE bf16 [B][n_query_tokens][Hq][d], on 16 bytes; lse: DEVICE fp32 [B][n_query_tokens][Hq] or NULL.
  *   KVE_ERR_STATE without kvE_attach_q4, KVE_ERR_CAPACITY if n_query_tokens exceeds max_query_tokens. */
 int kvE_decode_attn_q4(kvE_store* st, int layer, const void* q, int n_query_tokens, int dense, int causal, void* out, float* lse,

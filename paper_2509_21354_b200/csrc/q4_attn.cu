@@ -37,7 +37,7 @@ constexpr int QA_ROWS4 = 2 * Q4_UNIT_ROWS, QA_ROWS16 = 8;    // rows of a tile o
 static_assert(QA_ROWS16 * ROW_BYTES <= QA_V_OFF, "eight bf16 rows fit a stage");
 constexpr float QA_SLACK = 8.f;                              // by how much (log2) a logit may pass the softmax reference
 constexpr int QA_PLAN = 128;                                 // tiles looked up ahead of the copies
-constexpr int QA_NEW = 1, QA_FLUSH = 2, QA_END = 4;          // first, last tile of a sequence for this warp; nothing comes after it
+constexpr int QA_NEW = 1 << 16, QA_FLUSH = 2 << 16, QA_END = 4 << 16;          // first, last tile of a sequence for this warp; nothing comes after it
 
 struct Q4AttnArgs {
   LayerView v;
@@ -260,7 +260,7 @@ __global__ void __launch_bounds__(QaShape<NT, DUO>::WARPS * 32, 1) kve_decode_at
     // the next entries, up to 32 of one sequence, a lane each
     auto look_up = [&]() {
       const int jj = j + lane, at = pos_in + lane, count = min(32, n_entries - pos_in);
-      int4 e = make_int4(0, 0, 0, 0);      // page, first row in it, rows (negative: bf16 ones; 0: none), flags and the position of the first row
+      int4 e = make_int4(0, 0, 0, 0);      // page; first row in it, flags above; rows (negative: bf16 ones; 0: none); position of the first row
       if (jj < j_end) {
         const long long sb = (long long)x * v.max_chunks;
         const int of = jj < e0 ? jj : (jj < e1 ? jj - e0 : (jj < e2 ? jj - e1 : jj - e2));      // in its list
@@ -276,10 +276,10 @@ __global__ void __launch_bounds__(QaShape<NT, DUO>::WARPS * 32, 1) kve_decode_at
         e.x = page;
         e.y = within * (in4 ? QA_ROWS4 : QA_ROWS16);
         e.z = in4 ? min(QA_ROWS4, v.C - e.y) : -(jj < e2 ? QA_ROWS16 : min(QA_ROWS16, tail - of * QA_ROWS16));
-        e.w = (chunk * v.C + e.y) << 3;
+        e.w = chunk * v.C + e.y;
       }
       const bool last = at + CW >= n_entries;
-      e.w |= (at < CW ? QA_NEW : 0) | (last ? QA_FLUSH : 0) | (last && x == x1 ? QA_END : 0);
+      e.y |= (at < CW ? QA_NEW : 0) | (last ? QA_FLUSH : 0) | (last && x == x1 ? QA_END : 0);
       if (lane < count) plan[(planned + lane) % QA_PLAN] = e;
       planned += count;
       pos_in += count;
@@ -321,7 +321,7 @@ __global__ void __launch_bounds__(QaShape<NT, DUO>::WARPS * 32, 1) kve_decode_at
         if (e.z != 0) {
           unsigned char* dst = smem + (w * STAGES + stage) * QA_TILE_BYTES;
           const bool in4 = e.z > 0;
-          const long long row = (long long)e.x * v.C + e.y;
+          const long long row = (long long)e.x * v.C + (e.y & 0xffff);
           if (in4) {
             const uint32_t bytes = (uint32_t)e.z * (Q4_PAIR_BYTES / Q4_UNIT_ROWS);
             mbar_arrive_expect_tx(&my_full[stage], bytes);      // release: whoever sees the phase sees the description
@@ -338,8 +338,8 @@ __global__ void __launch_bounds__(QaShape<NT, DUO>::WARPS * 32, 1) kve_decode_at
         ++pushed;
         entry += CW;
         __threadfence_block();
-        progress[w] = active && (e.w & QA_END) ? 0x7fffffff : entry;      // (the planner may write over what this lane has read)
-        active = (e.w & QA_END) == 0;
+        progress[w] = active && (e.y & QA_END) ? 0x7fffffff : entry;      // (the planner may write over what this lane has read)
+        active = (e.y & QA_END) == 0;
       }
       if (__any_sync(0xffffffffu, ready)) {
         idle = 0;
@@ -735,23 +735,23 @@ __global__ void __launch_bounds__(QaShape<NT, DUO>::WARPS * 32, 1) kve_decode_at
       const unsigned char* base = smem + (warp * STAGES + stage) * QA_TILE_BYTES;
       const int4 what = infos[warp * STAGES + stage];
       if (a.causal) n = progress[CW + 1];
-      if (what.w & QA_NEW) {      // its query rows were brought when the sequence two before it was merged, which this warp has waited for
+      if (what.y & QA_NEW) {      // its query rows were brought when the sequence two before it was merged, which this warp has waited for
         start(nth & 1);
         ++nth;
       }
       if (what.z == QA_ROWS4) packed_rows(std::integral_constant<int, 2>(), base);
       else if (what.z > 0) packed_rows(std::integral_constant<int, 1>(), base);      // (the end of a chunk that is not a multiple of 32)
-      else if (what.z < 0) bf16_rows(-what.z, what.w >> 3, base);
+      else if (what.z < 0) bf16_rows(-what.z, what.w, base);
       __syncwarp();
       if (lane == 0) mbar_arrive(&my_empty[stage]);
-      if (what.w & QA_FLUSH) {
+      if (what.y & QA_FLUSH) {
         // the states of the sequence before are done with
         if (nth >= 2 && !mbar_wait_bounded(merged, (uint32_t)(nth - 2) & 1u)) {
           if (lane == 0) set_status(v.status, ERR_TIMEOUT);
           break;
         }
         leave();
-        if (what.w & QA_END) break;
+        if (what.y & QA_END) break;
         if (lane == 0) mbar_arrive(left);      // release
       }
       if (++stage == STAGES) { stage = 0; phase ^= 1u; }

@@ -218,6 +218,11 @@ CASES = [  # what the store holds, what is asked for
     (dict(n=20000, C_=64, W=100, Hkv=1, G=2), dict(dense=True)),                       # cut along the sequence
     (dict(n=20011, C_=128, W=1000, Hkv=2, G=4, listed=100, keep=lambda s, t: t % 2 == s), {}),
     (dict(n=200, C_=16, W=4, B=40, Hkv=16), dict(dense=True)),                         # many sequences
+    (dict(n=70, C_=16, W=4, B=100, Hkv=3, G=2, listed=4, keep=lambda s, t: (s * 7 + t) % 4 < s % 4), {}),      # CTAs that go from one to the next, with few rows and none kept
+    (dict(n=333, C_=64, W=30, B=20, Hkv=8, G=7, listed=4, keep=every_third), {}),
+    (dict(n=333, C_=32, W=30, B=20, Hkv=8, G=3, T=4), dict(dense=True, causal=True)),
+    (dict(n=90, C_=16, W=40, B=6, Hkv=30, G=1, T=40), dict(dense=True, causal=True)),  # 40 query rows: three groups
+    (dict(n=3, C_=16, W=1, B=200, Hkv=1, G=1), {}),
 ]
 
 
@@ -243,6 +248,28 @@ def test_large_logits_and_offsets():
     rising = ref.bits((np.linspace(0, 8, 700)[None, :, None] * np.ones((2, 1, 128))).astype(np.float32))      # the largest logit comes last
     case = Case(n=700, W=50, K=from_bits(rising))
     case.check(q=torch.ones((1, 1, 2, 128), dtype=torch.bfloat16, device="cuda"), dense=True)
+
+
+@pytest.mark.parametrize("G", [1, 8, 16])
+@pytest.mark.parametrize("sizes", [(1e-12, 1e-12), (1e12, 1e12), (1e-9, 1e9), (1e9, 1e-9)])
+def test_values_of_any_size(G, sizes):
+    """packed values, and bf16 ones beside them, of other sizes than 1; scales that grow and shrink along the sequence"""
+    rng = np.random.default_rng(5)
+    V = rng.standard_normal((2, 700, 128))
+    V[:, :640] *= sizes[0] * np.exp2(rng.integers(-6, 7, size=(2, 10, 1))).repeat(64, axis=1)
+    V[:, 640:] *= sizes[1]
+    V[:, :, 64:] *= 1e-3
+    case = Case(n=700, W=60, G=G, V=from_bits(ref.bits(V.astype(np.float32))))
+    case.check(dense=True)
+
+
+def test_queries_of_any_size():
+    """each query row has a power of two of its own"""
+    case = Case(n=500, G=4, B=1, Hkv=2)
+    q = normal((1, 1, 8, 128), 3)
+    q = (q.float() * torch.tensor([1e-20, 1.0, 1e4, 1e-3, 3e-39, 0.0, 1e2, 1e-8], device="cuda").view(1, 1, 8, 1)).to(torch.bfloat16)
+    q[0, 0, 1, 5:] *= 1e-6
+    case.check(q=q, dense=True)
 
 
 def test_infinite_and_nan_rows():
