@@ -11,7 +11,7 @@
 //  * both products are m16n8k16 MMAs with the cache on the M side (keys: 16 rows; values, transposed: 16 dims) and the queries in the
 //    eight columns.  The logits' accumulator becomes the weights' operand through movmatrix, in registers.
 //  * up to four query rows: the eight columns are the four rows twice, once for either group of 64 dims (q is zero in the other half; the weights have the
-//    group's scale), so that a lane has to do with one group only: half of the scales, weights and conversions (see DUO).
+//    group's scale), so that a lane has to do with one group only: half of the scales, weights and conversions.
 //  * the weights p s F of packed rows are fp16: 11 bits, whose rounding (2^-12 a row) stays far below the result's own (2^-9).  F, a power of two per
 //    warp and group, follows the largest p s so that they neither overflow nor run out of bits.  bf16 rows take their weights as two bf16 planes.
 //  * a tile's products with the values are summed from zero and added to the accumulator by ordinary additions: the tensor core cuts off what lies below
@@ -53,15 +53,18 @@ struct Q4AttnArgs {
   int32_t* counters;    // [S][groups], zero between launches
 };
 
-template <int NT, bool DUO> struct QaShape {
-  static constexpr int MCOLS = 8 * NT, COLS = DUO ? 4 : MCOLS;      // columns of the MMAs; query rows of a CTA
-  static constexpr int CW = NT == 1 ? 12 : 8;                // consumer warps
+// COLS_: query rows of a CTA, 4, 8 or 16
+template <int COLS_> struct QaShape {
+  static constexpr int COLS = COLS_;
+  static constexpr bool MANY = COLS == 16;
+  static constexpr int QROWS = MANY ? 16 : 8;                // rows of fp16 queries (four of them twice)
+  static constexpr int CW = MANY ? 8 : 12;                   // consumer warps
   static constexpr int PRODUCERS = 2, PLANNER = CW + PRODUCERS, MERGER = PLANNER + 1, WARPS = MERGER + 1;
   static constexpr int STAGES = 3;                           // per consumer
   static constexpr int OFF_STATE = CW * STAGES * QA_TILE_BYTES;                          // [consumers][query rows][132]: behind the ring
   static constexpr int OFF_Q = OFF_STATE + CW * COLS * ATTN_PARTIAL_FLOATS * 4;          // [2][query rows][128] bf16; the same as fp16; what undoes their powers of two: [2][query rows]
   static constexpr int OFF_QH = OFF_Q + 2 * COLS * ROW_BYTES;
-  static constexpr int OFF_UNDO = OFF_QH + 2 * MCOLS * ROW_BYTES;
+  static constexpr int OFF_UNDO = OFF_QH + 2 * QROWS * ROW_BYTES;
   static constexpr int OFF_INFO = OFF_UNDO + 2 * COLS * 4;   // [consumers][stages] int4: the tile's entry of the table
   static constexpr int OFF_PLAN = OFF_INFO + CW * STAGES * 16;      // [QA_PLAN] int4: tiles looked up
   static constexpr int OFF_BAR = OFF_PLAN + QA_PLAN * 16;
@@ -73,6 +76,11 @@ __device__ __forceinline__ int load_now(const int32_t* p) { return *reinterpret_
 __device__ __forceinline__ float2 f16_pair(uint32_t w) {
   float2 d;
   asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.f32.f16 %0, a;\n\tcvt.f32.f16 %1, b;\n\t}" : "=f"(d.x), "=f"(d.y) : "r"(w));
+  return d;
+}
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("max.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
   return d;
 }
 __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
@@ -121,13 +129,11 @@ __device__ __forceinline__ void write_row(const Q4AttnArgs& a, int s, int rr, fl
 __device__ __forceinline__ uint32_t qa_begin(uint32_t c, uint32_t I, uint32_t P) { return (c * I) / P; }
 __device__ __forceinline__ uint32_t qa_owner(uint32_t x, uint32_t I, uint32_t P) { return ((x + 1u) * P - 1u) / I; }
 
-// NT: column tiles of eight query rows.  DUO (NT == 1): up to four query rows; columns 4 to 7 are columns 0 to 3 again, where the MMAs with packed rows have group 0
-// in the columns below 4 and group 1 in those from 4 on
-template <int NT, bool DUO>
-__global__ void __launch_bounds__(QaShape<NT, DUO>::WARPS * 32, 1) kve_decode_attn_q4_kernel(Q4AttnArgs a) {
-  using Shape = QaShape<NT, DUO>;
-  constexpr int STAGES = Shape::STAGES, CW = Shape::CW, WARPS = Shape::WARPS, COLS = Shape::COLS, MCOLS = Shape::MCOLS;
-  constexpr int NG = DUO ? 1 : 2;      // groups that a lane has to do with
+template <int COLS>
+__global__ void __launch_bounds__(QaShape<COLS>::WARPS * 32, 1) kve_decode_attn_q4_kernel(Q4AttnArgs a) {
+  using Shape = QaShape<COLS>;
+  constexpr int STAGES = Shape::STAGES, CW = Shape::CW, WARPS = Shape::WARPS;
+  constexpr bool MANY = Shape::MANY, DUO = COLS == 4;
   extern __shared__ __align__(128) unsigned char smem[];
   const LayerView& v = a.v;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g8 = lane >> 2, t4 = lane & 3;
@@ -165,8 +171,8 @@ __global__ void __launch_bounds__(QaShape<NT, DUO>::WARPS * 32, 1) kve_decode_at
 
   // ---- a warp brings the query rows of sequence s into slot `slot`: bf16, and fp16 times a power of two ----
   auto fetch_queries = [&](int s, int slot) {
-    uint32_t* Qh = reinterpret_cast<uint32_t*>(smem + Shape::OFF_QH) + slot * MCOLS * 64;
-    uint4* Qb = reinterpret_cast<uint4*>(smem + Shape::OFF_Q) + slot * COLS * 16;
+    uint32_t* Qh = reinterpret_cast<uint32_t*>(smem + Shape::OFF_QH) + slot * Shape::QROWS * 64;
+    uint32_t* Qb = reinterpret_cast<uint32_t*>(smem + Shape::OFF_Q) + slot * COLS * 64;
     float* q_undo = reinterpret_cast<float*>(smem + Shape::OFF_UNDO) + slot * COLS;
     const int b = (int)a.by_h.div((uint32_t)s), h = s - b * v.H, piece = lane & 15;
 #pragma unroll 4
@@ -176,8 +182,11 @@ __global__ void __launch_bounds__(QaShape<NT, DUO>::WARPS * 32, 1) kve_decode_at
         const int t = (int)a.by_g.div((uint32_t)(row0 + c)), gq = row0 + c - t * a.G;
         w = __ldcg(reinterpret_cast<const uint4*>(a.q + ((((long long)b * a.T + t) * v.H + h) * a.G + gq) * D + piece * 8));
       }
-      Qb[c * 16 + piece] = w;
       const uint32_t word[4] = {w.x, w.y, w.z, w.w};
+      // where pair e of the piece lies: row by row, or (MANY) as the operand registers of the eight products along a row, four of each lane
+      auto place = [&](int e) { return MANY ? (((piece >> 2) * 2 + (e >> 1)) * 32 + (c & 7) * 4 + (piece & 3)) * 4 + (c >> 3) + 2 * (e & 1) : c * 64 + piece * 4 + e; };
+#pragma unroll
+      for (int e = 0; e < 4; ++e) Qb[place(e)] = word[e];
       float most = 0.f;      // of the finite ones
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -196,7 +205,7 @@ __global__ void __launch_bounds__(QaShape<NT, DUO>::WARPS * 32, 1) kve_decode_at
           Qh[c * 64 + piece * 4 + e] = piece < 8 ? w16 : 0u;
           Qh[(c + 4) * 64 + piece * 4 + e] = piece < 8 ? 0u : w16;
         } else {
-          Qh[c * 64 + piece * 4 + e] = w16;
+          Qh[place(e)] = w16;
         }
       }
       if (piece == 0) q_undo[c] = __uint_as_float((uint32_t)(127 - power) << 23);
@@ -373,388 +382,671 @@ __global__ void __launch_bounds__(QaShape<NT, DUO>::WARPS * 32, 1) kve_decode_at
     }
   } else {
     // ================= consumers =================
-    // ---- the sequence under way ----
-    const uint16_t *Qh = nullptr, *Qb = nullptr;      // its query rows, as fp16 and as bf16
-    // column nt 8 + g8: the numbers 32 j + 8 t4 .. + 7, as fp16 (from shared memory every time)
-    auto q_half = [&](int nt, int j) { return *reinterpret_cast<const uint4*>(Qh + (nt * 8 + g8) * D + 32 * j + 8 * t4); };
-    float undo[NT][2], qsum[NT][NG][2];     // per column 2 t4, 2 t4 + 1: what takes q's power of two off a sum of codes (2^-24) and makes it a log2 logit; sums of q over the groups
-    int n = 0;                              // tokens stored (read where it matters)
-    auto row_of = [&](int nt, int c) { return nt * 8 + (DUO ? c & 3 : c); };      // the query row of a column
-    auto last_pos = [&](int nt, int x) {    // causal: the last position a column sees
-      return a.causal ? n - a.T + (int)a.by_g.div((uint32_t)min(row0 + row_of(nt, 2 * t4 + x), R - 1)) : 0x7fffffff;
-    };
-
-    float acc[NT][8][4];           // [m]: dims d = 64 (m / 4) + 8 g8 + 2 (m % 4) and d + 1, columns 2 t4 and 2 t4 + 1: (d, c), (d, c + 1), times F 2^-24; (d + 1, c), (d + 1, c + 1), times F 2^-20
-    float l[NT][2], zs[NT][NG][2]; // this lane's rows' share, per column: sum of weights; of weights times what code 0 stands for
-    // per column: the softmax's reference (0 until there is one), and what a logit may exceed it by (-inf until there is one)
-    float ref[NT][2], over_by[NT][2];
-    float F[NG];     // weight factor of a group: the largest p s so far times F lies in [2^6, 2^7); a scale with s F > 2^7 asks for another
-      // (2^64 at most, and to begin with: sums of bf16 rows times F stay finite below |v| = 2^60)
-    // a fresh state, and the query rows in slot `slot`
-    auto start = [&](int slot) {
-      Qh = reinterpret_cast<const uint16_t*>(smem + Shape::OFF_QH) + slot * MCOLS * D;
-      Qb = reinterpret_cast<const uint16_t*>(smem + Shape::OFF_Q) + slot * COLS * D;
-      const float* q_undo = reinterpret_cast<const float*>(smem + Shape::OFF_UNDO) + slot * COLS;
-#pragma unroll
-      for (int g = 0; g < NG; ++g) F[g] = 0x1p64f;
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        float sum[NG] = {};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const uint4 w = q_half(nt, j);
-          const float2 e0 = f16_pair(w.x), e1 = f16_pair(w.y), e2 = f16_pair(w.z), e3 = f16_pair(w.w);
-          sum[DUO ? 0 : j >> 1] += (e0.x + e0.y) + (e2.x + e2.y) + 16.f * ((e1.x + e1.y) + (e3.x + e3.y));
+    // goes through this warp's tiles: start(slot) at the first of a sequence, packed rows, bf16 rows, leave() at the last
+    auto consume = [&](auto&& start, auto&& packed_rows, auto&& bf16_rows, auto&& leave) {
+      uint64_t *my_full = full + warp * STAGES, *my_empty = empty + warp * STAGES;
+      int nth = 0, stage = 0;      // sequences begun; stage of the next tile
+      uint32_t phase = 0;
+      bool ok = mbar_wait_bounded(fetched, 0);
+      if (!ok && lane == 0) set_status(v.status, ERR_TIMEOUT);
+      while (ok) {
+        if (!mbar_wait_bounded(&my_full[stage], phase)) {
+          if (lane == 0) set_status(v.status, ERR_TIMEOUT);
+          break;
         }
-        const float off = q_undo[row_of(nt, g8)] * sl2;
-#pragma unroll
-        for (int h = 0; h < NG; ++h) {
-          float y = sum[h];
-          y += __shfl_xor_sync(0xffffffffu, y, 1);
-          y += __shfl_xor_sync(0xffffffffu, y, 2);      // of column g8, in its four lanes
-          y *= off;
-          qsum[nt][h][0] = __shfl_sync(0xffffffffu, y, 8 * t4);
-          qsum[nt][h][1] = __shfl_sync(0xffffffffu, y, 8 * t4 + 4);
+        const unsigned char* base = smem + (warp * STAGES + stage) * QA_TILE_BYTES;
+        const int4 what = infos[warp * STAGES + stage];
+        if (what.y & QA_NEW) {      // its query rows were brought when the sequence two before it was merged, which this warp has waited for
+          start(nth & 1);
+          ++nth;
         }
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          undo[nt][c] = q_undo[row_of(nt, 2 * t4 + c)] * 0x1p12f * sl2 * 0x1p12f;
-          ref[nt][c] = 0.f; over_by[nt][c] = -INFINITY; l[nt][c] = 0.f;
-#pragma unroll
-          for (int g = 0; g < NG; ++g) zs[nt][g][c] = 0.f;
+        if (what.z > 0) packed_rows(what.z, base);
+        else if (what.z < 0) bf16_rows(-what.z, what.w, base);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&my_empty[stage]);
+        if (what.y & QA_FLUSH) {
+          // the states of the sequence before are done with
+          if (nth >= 2 && !mbar_wait_bounded(merged, (uint32_t)(nth - 2) & 1u)) {
+            if (lane == 0) set_status(v.status, ERR_TIMEOUT);
+            break;
+          }
+          leave();
+          if (what.y & QA_END) break;
+          if (lane == 0) mbar_arrive(left);      // release
         }
-#pragma unroll
-        for (int m = 0; m < 8; ++m)
-#pragma unroll
-          for (int y = 0; y < 4; ++y) acc[nt][m][y] = 0.f;
+        if (++stage == STAGES) { stage = 0; phase ^= 1u; }
       }
     };
+    if constexpr (!MANY) {
+      // ---- up to eight query rows: the cache on the M side, the queries in the columns.  Up to four (DUO): rows 0 to 3 twice, where the products with packed keys and
+      // values have group 0 in the columns below 4 and group 1 in those from 4 on ----
+      constexpr int NT = 1, NG = DUO ? 1 : 2;      // groups that a lane has to do with
+      const uint16_t *Qh = nullptr, *Qb = nullptr;      // its query rows, as fp16 and as bf16
+      // column nt 8 + g8: the numbers 32 j + 8 t4 .. + 7, as fp16 (from shared memory every time)
+      auto q_half = [&](int nt, int j) { return *reinterpret_cast<const uint4*>(Qh + (nt * 8 + g8) * D + 32 * j + 8 * t4); };
+      float undo[NT][2], qsum[NT][NG][2];     // per column 2 t4, 2 t4 + 1: what takes q's power of two off a sum of codes (2^-24) and makes it a log2 logit; sums of q over the groups
+      auto row_of = [&](int nt, int c) { return nt * 8 + (DUO ? c & 3 : c); };      // the query row of a column
+      auto last_pos = [&](int nt, int x) {    // causal: the last position a column sees
+        return a.causal ? progress[CW + 1] - a.T + (int)a.by_g.div((uint32_t)min(row0 + row_of(nt, 2 * t4 + x), R - 1)) : 0x7fffffff;
+      };
 
-    // Logits minus reference (log2 units; of each of this lane's rows: c, c + 1) to weights in place.  s: the largest scale of
-    // these rows in either group.  Raises reference and factors where it has to.
-    auto weigh = [&](auto& x, float s0, float s1) {
-      constexpr int N = (int)(sizeof(x[0]) / sizeof(float));
-      bool over = false;
+      float acc[NT][8][4];           // [m]: dims d = 64 (m / 4) + 8 g8 + 2 (m % 4) and d + 1, columns 2 t4 and 2 t4 + 1: (d, c), (d, c + 1), times F 2^-24; (d + 1, c), (d + 1, c + 1), times F 2^-20
+      float l[NT][2], zs[NT][NG][2]; // this lane's rows' share, per column: sum of weights; of weights times what code 0 stands for
+      // per column: the softmax's reference (0 until there is one), and what a logit may exceed it by (-inf until there is one)
+      float ref[NT][2], over_by[NT][2];
+      float F[NG];     // weight factor of a group: the largest p s so far times F lies in [2^6, 2^7); a scale with s F > 2^7 asks for another
+        // (2^64 at most, and to begin with: sums of bf16 rows times F stay finite below |v| = 2^60)
+      // a fresh state, and the query rows in slot `slot`
+      auto start = [&](int slot) {
+        Qh = reinterpret_cast<const uint16_t*>(smem + Shape::OFF_QH) + slot * Shape::QROWS * D;
+        Qb = reinterpret_cast<const uint16_t*>(smem + Shape::OFF_Q) + slot * COLS * D;
+        const float* q_undo = reinterpret_cast<const float*>(smem + Shape::OFF_UNDO) + slot * COLS;
 #pragma unroll
-      for (int g = 0; g < NG; ++g) over |= (g ? s1 : s0) * F[g] > 128.f;
+        for (int g = 0; g < NG; ++g) F[g] = 0x1p64f;
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+        for (int nt = 0; nt < NT; ++nt) {
+          float sum[NG] = {};
 #pragma unroll
-        for (int i = 0; i < N; ++i) over |= x[nt][i] > over_by[nt][i & 1];
-      if (__any_sync(0xffffffffu, over)) {
-        float most = 0.f;      // of the factors that the sums so far get
+          for (int j = 0; j < 4; ++j) {
+            const uint4 w = q_half(nt, j);
+            const float2 e0 = f16_pair(w.x), e1 = f16_pair(w.y), e2 = f16_pair(w.z), e3 = f16_pair(w.w);
+            sum[DUO ? 0 : j >> 1] += (e0.x + e0.y) + (e2.x + e2.y) + 16.f * ((e1.x + e1.y) + (e3.x + e3.y));
+          }
+          const float off = q_undo[row_of(nt, g8)] * sl2;
+#pragma unroll
+          for (int h = 0; h < NG; ++h) {
+            float y = sum[h];
+            y += __shfl_xor_sync(0xffffffffu, y, 1);
+            y += __shfl_xor_sync(0xffffffffu, y, 2);      // of column g8, in its four lanes
+            y *= off;
+            qsum[nt][h][0] = __shfl_sync(0xffffffffu, y, 8 * t4);
+            qsum[nt][h][1] = __shfl_sync(0xffffffffu, y, 8 * t4 + 4);
+          }
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            undo[nt][c] = q_undo[row_of(nt, 2 * t4 + c)] * 0x1p12f * sl2 * 0x1p12f;
+            ref[nt][c] = 0.f; over_by[nt][c] = -INFINITY; l[nt][c] = 0.f;
+#pragma unroll
+            for (int g = 0; g < NG; ++g) zs[nt][g][c] = 0.f;
+          }
+#pragma unroll
+          for (int m = 0; m < 8; ++m)
+#pragma unroll
+            for (int y = 0; y < 4; ++y) acc[nt][m][y] = 0.f;
+        }
+      };
+
+      // Logits minus reference (log2 units; of each of this lane's rows: c, c + 1) to weights in place.  s: the largest scale of
+      // these rows in either group.  Raises reference and factors where it has to.
+      auto weigh = [&](auto& x, float s0, float s1) {
+        constexpr int N = (int)(sizeof(x[0]) / sizeof(float));
+        bool over = false;
+#pragma unroll
+        for (int g = 0; g < NG; ++g) over |= (g ? s1 : s0) * F[g] > 128.f;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int i = 0; i < N; ++i) over |= x[nt][i] > over_by[nt][i & 1];
+        if (__any_sync(0xffffffffu, over)) {
+          float most = 0.f;      // of the factors that the sums so far get
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              float top = x[nt][c];
+#pragma unroll
+              for (int i = c + 2; i < N; i += 2) top = fmaxf(top, x[nt][i]);
+#pragma unroll
+              for (int o = 4; o <= 16; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+              const bool first = over_by[nt][c] == -INFINITY;
+              const float to = ref[nt][c] + (first ? (top == -INFINITY ? 0.f : top) : fmaxf(top, 0.f)), up = to - ref[nt][c];
+              const float f = first ? 1.f : ex2_fast(-up);
+              most = fmaxf(most, f);
+              if (top != -INFINITY) over_by[nt][c] = QA_SLACK;
+              ref[nt][c] = to;
+#pragma unroll
+              for (int i = c; i < N; i += 2) x[nt][i] -= up;
+              l[nt][c] *= f;
+#pragma unroll
+              for (int g = 0; g < NG; ++g) zs[nt][g][c] *= f;
+#pragma unroll
+              for (int m = 0; m < 8; ++m) { acc[nt][m][c] *= f; acc[nt][m][2 + c] *= f; }
+            }
+          most = warp_max(most);
+#pragma unroll
+          for (int g = 0; g < NG; ++g) {
+            float largest = g ? s1 : s0;      // of the group: DUO has the other one in the lanes t4 ^ 2
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1)
+              if (!DUO || o != 2) largest = fmaxf(largest, __shfl_xor_sync(0xffffffffu, largest, o));
+            largest = fmaxf(64.f / F[g] * most, largest);
+            const int e = min(max((int)(__float_as_uint(largest) >> 23) - 127, -58), 126);
+            const float to = __uint_as_float((uint32_t)(127 + 6 - e) << 23), f = to / F[g];
+            F[g] = to;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int m = 0; m < (DUO ? 8 : 4); ++m)      // (DUO: what the lane holds of the other group's dims is nobody's)
+#pragma unroll
+                for (int y = 0; y < 4; ++y) acc[nt][4 * g + m][y] *= f;
+          }
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int i = 0; i < N; ++i) {
+            x[nt][i] = ex2_fast(x[nt][i]);
+            l[nt][i & 1] += x[nt][i];
+          }
+      };
+
+      auto add_to = [](float (&sum)[4], const float (&d)[4], float2 f01, float2 f23) {
+        const float2 p = fma2(make_float2(d[0], d[1]), f01, make_float2(sum[0], sum[1])), q = fma2(make_float2(d[2], d[3]), f23, make_float2(sum[2], sum[3]));
+        sum[0] = p.x; sum[1] = p.y; sum[2] = q.x; sum[3] = q.y;
+      };
+      // a tile of packed rows, UNITS times 16
+      auto packed_rows = [&](auto units, const unsigned char* base) {
+        constexpr int UNITS = decltype(units)::value;
+        float x[NT][4 * UNITS];
+        uint32_t va[UNITS][NG], vc[UNITS][NG];      // scale and lowest number of the rows g8 and g8 + 8, values
+        {
+          float d[UNITS][NT][2][4];      // two chains: the groups; DUO: even and odd words
+          uint4 ka[UNITS], kc[UNITS];
+#pragma unroll
+          for (int u = 0; u < UNITS; ++u) {
+            ka[u] = *reinterpret_cast<const uint4*>(base + u * Q4_PAIR_BYTES + lane * 16);
+            kc[u] = *reinterpret_cast<const uint4*>(base + u * Q4_PAIR_BYTES + 512 + lane * 16);
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            uint32_t pa[UNITS][4], pc[UNITS][4];
+#pragma unroll
+            for (int u = 0; u < UNITS; ++u) {
+              q4_spread(word_of(ka[u], j), pa[u]);
+              q4_spread(word_of(kc[u], j), pc[u]);
+            }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              const uint4 qw = q_half(nt, j);
+#pragma unroll
+              for (int u = 0; u < UNITS; ++u) {
+                const uint32_t A0[4] = {pa[u][0], pc[u][0], pa[u][1], pc[u][1]}, A1[4] = {pa[u][2], pc[u][2], pa[u][3], pc[u][3]};
+                float(&to)[4] = d[u][nt][DUO ? j & 1 : j >> 1];
+                if (DUO ? j < 2 : (j & 1) == 0) mma_f16_first(to, A0, qw.x, qw.y);
+                else mma_f16_next(to, A0, qw.x, qw.y);
+                mma_f16_next(to, A1, qw.z, qw.w);
+              }
+            }
+          }
+          // x = low + s c: the sum over a group is s (what the MMAs give) + low (sum of q)
+#pragma unroll
+          for (int u = 0; u < UNITS; ++u) {
+            const unsigned char* kh = base + u * Q4_PAIR_BYTES + Q4_CODE_BYTES + g8 * 8;
+            const unsigned char* vh = kh + Q4_UNIT_BYTES;
+            if constexpr (DUO) {
+              // a lane has the sum of its own group; the other group's is in the lane t4 ^ 2
+              const int of = (t4 >> 1) * 4;
+              const uint32_t ha = *reinterpret_cast<const uint32_t*>(kh + of), hc = *reinterpret_cast<const uint32_t*>(kh + 64 + of);
+              const float sa = bf16lo(ha), sc = bf16lo(hc), la = bf16hi(ha), lc = bf16hi(hc);
+#pragma unroll
+              for (int c = 0; c < 2; ++c) {
+                const float(&y)[2][4] = d[u][0];
+                const float half_ref = -0.5f * ref[0][c];
+                const float p = fmaf((y[0][c] + y[1][c]) * sa, undo[0][c], fmaf(la, qsum[0][0][c], half_ref));
+                const float q = fmaf((y[0][2 + c] + y[1][2 + c]) * sc, undo[0][c], fmaf(lc, qsum[0][0][c], half_ref));
+                x[0][4 * u + c] = p + __shfl_xor_sync(0xffffffffu, p, 2);
+                x[0][4 * u + 2 + c] = q + __shfl_xor_sync(0xffffffffu, q, 2);
+              }
+              va[u][0] = *reinterpret_cast<const uint32_t*>(vh + of);
+              vc[u][0] = *reinterpret_cast<const uint32_t*>(vh + 64 + of);
+            } else {
+              const uint2 ha = *reinterpret_cast<const uint2*>(kh), hc = *reinterpret_cast<const uint2*>(kh + 64), wa = *reinterpret_cast<const uint2*>(vh), wc = *reinterpret_cast<const uint2*>(vh + 64);
+              const float sa0 = bf16lo(ha.x), sa1 = bf16lo(ha.y), sc0 = bf16lo(hc.x), sc1 = bf16lo(hc.y);
+              const float la0 = bf16hi(ha.x), la1 = bf16hi(ha.y), lc0 = bf16hi(hc.x), lc1 = bf16hi(hc.y);
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                  const float(&y)[2][4] = d[u][nt];
+                  x[nt][4 * u + c] = fmaf(fmaf(y[0][c], sa0, y[1][c] * sa1), undo[nt][c], fmaf(la0, qsum[nt][0][c], fmaf(la1, qsum[nt][NG - 1][c], -ref[nt][c])));
+                  x[nt][4 * u + 2 + c] = fmaf(fmaf(y[0][2 + c], sc0, y[1][2 + c] * sc1), undo[nt][c], fmaf(lc0, qsum[nt][0][c], fmaf(lc1, qsum[nt][NG - 1][c], -ref[nt][c])));
+                }
+              va[u][0] = wa.x; va[u][NG - 1] = wa.y;
+              vc[u][0] = wc.x; vc[u][NG - 1] = wc.y;
+            }
+          }
+        }
+        float most[NG] = {};
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u)
+#pragma unroll
+          for (int g = 0; g < NG; ++g) most[g] = fmaxf(most[g], fmaxf(bf16lo(va[u][g]), bf16lo(vc[u][g])));
+        weigh(x, most[0], most[NG - 1]);
+        uint32_t b[NG][UNITS][NT][2];      // weights times scale: MMA operands
+#pragma unroll
+        for (int g = 0; g < NG; ++g)
+#pragma unroll
+          for (int u = 0; u < UNITS; ++u) {
+            const float f_a = bf16lo(va[u][g]) * F[g], f_c = bf16lo(vc[u][g]) * F[g], l_a = bf16hi(va[u][g]), l_c = bf16hi(vc[u][g]);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              const float* p = &x[nt][4 * u];
+              b[g][u][nt][0] = transpose_8x8(pack_f16x2(p[0] * f_a, p[1] * f_a));
+              b[g][u][nt][1] = transpose_8x8(pack_f16x2(p[2] * f_c, p[3] * f_c));
+#pragma unroll
+              for (int c = 0; c < 2; ++c) zs[nt][g][c] = fmaf(p[c], l_a, fmaf(p[2 + c], l_c, zs[nt][g][c]));
+            }
+          }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int g = DUO ? 0 : h;
+          uint4 vw[UNITS];
+#pragma unroll
+          for (int u = 0; u < UNITS; ++u) vw[u] = *reinterpret_cast<const uint4*>(base + u * Q4_PAIR_BYTES + Q4_UNIT_BYTES + h * 512 + lane * 16);
+#pragma unroll
+          for (int m = 0; m < 4; ++m) {
+            float d[NT][4];
+#pragma unroll
+            for (int u = 0; u < UNITS; ++u) {
+              uint32_t A[4];
+              q4_spread(word_of(vw[u], m), A);
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) {
+                if (u == 0) mma_f16_first(d[nt], A, b[g][u][nt][0], b[g][u][nt][1]);
+                else mma_f16_next(d[nt], A, b[g][u][nt][0], b[g][u][nt][1]);
+              }
+            }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) add_to(acc[nt][4 * h + m], d[nt], make_float2(1.f, 1.f), make_float2(1.f, 1.f));
+          }
+        }
+      };
+
+      // a tile of `rows` <= 8 bf16 rows, the first at position pos
+      auto bf16_rows = [&](int rows, int pos, const unsigned char* base) {
+        float x[NT][2];
+        {
+          float d[NT][2][4];
+          const uint4* kr = reinterpret_cast<const uint4*>(base + g8 * ROW_BYTES) + t4;
+#pragma unroll
+          for (int jw = 0; jw < 4; ++jw) {
+            const uint4 kw = kr[4 * jw];
+            const uint32_t A0[4] = {kw.x, 0u, kw.y, 0u}, A1[4] = {kw.z, 0u, kw.w, 0u};
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              const uint4 qw = *reinterpret_cast<const uint4*>(Qb + row_of(nt, g8) * D + 32 * jw + 8 * t4);
+              if ((jw & 1) == 0) mma_bf16_first(d[nt][jw >> 1], A0, qw.x, qw.y);
+              else mma_bf16_next(d[nt][jw >> 1], A0, qw.x, qw.y);
+              mma_bf16_next(d[nt][jw >> 1], A1, qw.z, qw.w);
+            }
+          }
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) x[nt][c] = fmaf(d[nt][0][c] + d[nt][1][c], sl2, -ref[nt][c]);
+          if (rows < QA_ROWS16 || a.causal) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int c = 0; c < 2; ++c)
+                if (g8 >= rows || pos + g8 > last_pos(nt, c)) x[nt][c] = -INFINITY;
+          }
+        }
+        uint4 e[2], o[2];      // this lane's numbers of the rows 2 t4 and 2 t4 + 1
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          e[h] = *reinterpret_cast<const uint4*>(base + QA_V_OFF + 2 * t4 * ROW_BYTES + h * 128 + g8 * 16);
+          o[h] = *reinterpret_cast<const uint4*>(base + QA_V_OFF + (2 * t4 + 1) * ROW_BYTES + h * 128 + g8 * 16);
+        }
+        if (rows < QA_ROWS16) {      // what an earlier tile left there may be anything
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if (2 * t4 >= rows) e[h] = make_uint4(0u, 0u, 0u, 0u);
+            if (2 * t4 + 1 >= rows) o[h] = make_uint4(0u, 0u, 0u, 0u);
+          }
+        }
+        weigh(x, 0.f, 0.f);
+        // both planes of the weights in one MMA: rows 0-7 of its contraction have the first, rows 8-15, the same rows again, the second
+        uint32_t b[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          const uint32_t hi = pack_bf16x2(x[nt][0], x[nt][1]);
+          b[nt][0] = transpose_8x8(hi);
+          b[nt][1] = transpose_8x8(pack_bf16x2(x[nt][0] - bf16lo(hi), x[nt][1] - bf16hi(hi)));
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t ew[4] = {e[h].x, e[h].y, e[h].z, e[h].w}, ow[4] = {o[h].x, o[h].y, o[h].z, o[h].w};
+          const float f01 = F[DUO ? 0 : h] * 0x1p-24f, f23 = F[DUO ? 0 : h] * 0x1p-20f;
+#pragma unroll
+          for (int m = 0; m < 4; ++m) {
+            const uint32_t a0 = __byte_perm(ew[m], ow[m], 0x5410), a1 = __byte_perm(ew[m], ow[m], 0x7632);
+            const uint32_t A[4] = {a0, a1, a0, a1};
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              float d[4];
+              mma_bf16_first(d, A, b[nt][0], b[nt][1]);
+              add_to(acc[nt][4 * h + m], d, make_float2(f01, f01), make_float2(f23, f23));
+            }
+          }
+        }
+      };
+
+      // leaves the state of the sequence in shared memory
+      auto leave = [&]() {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int o = 4; o <= 16; o <<= 1) {
+              l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], o);
+#pragma unroll
+              for (int g = 0; g < NG; ++g) zs[nt][g][c] += __shfl_xor_sync(0xffffffffu, zs[nt][g][c], o);
+            }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
-            float top = x[nt][c];
+            float* st = states + (warp * COLS + row_of(nt, 2 * t4 + c)) * ATTN_PARTIAL_FLOATS;
 #pragma unroll
-            for (int i = c + 2; i < N; i += 2) top = fmaxf(top, x[nt][i]);
+            for (int g = 0; g < NG; ++g) {
+              const float zv = zs[nt][g][c], un = 1.f / F[g];
+              float* o = st + 64 * (DUO ? t4 >> 1 : g) + 8 * g8;
+              float y[8];
 #pragma unroll
-            for (int o = 4; o <= 16; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-            const bool first = over_by[nt][c] == -INFINITY;
-            const float to = ref[nt][c] + (first ? (top == -INFINITY ? 0.f : top) : fmaxf(top, 0.f)), up = to - ref[nt][c];
+              for (int m = 0; m < 4; ++m) {
+                const float even = DUO && t4 >= 2 ? acc[nt][4 + m][c] : acc[nt][4 * g + m][c], odd = DUO && t4 >= 2 ? acc[nt][4 + m][2 + c] : acc[nt][4 * g + m][2 + c];
+                y[2 * m] = fmaf(even * 0x1p24f, un, zv);
+                y[2 * m + 1] = fmaf(odd * 0x1p20f, un, zv);
+              }
+              *reinterpret_cast<float4*>(o) = make_float4(y[0], y[1], y[2], y[3]);
+              *reinterpret_cast<float4*>(o + 4) = make_float4(y[4], y[5], y[6], y[7]);
+            }
+            if (g8 == 0 && (!DUO || t4 < 2)) { st[128] = over_by[nt][c] == -INFINITY ? -INFINITY : ref[nt][c]; st[129] = l[nt][c]; }
+          }
+        __syncwarp();
+      };
+
+      consume(start, [&](int rows, const unsigned char* base) {
+        if (rows == QA_ROWS4) packed_rows(std::integral_constant<int, 2>(), base);
+        else packed_rows(std::integral_constant<int, 1>(), base);      // (the end of a chunk that is not a multiple of 32)
+      }, bf16_rows, leave);
+    } else {
+      // ---- up to sixteen query rows: the queries on the M side of both products, so that the logits' accumulator is the weights' operand as it stands.  A lane has the
+      // query rows g8 and g8 + 8 and two keys of every eight ----
+      const uint4 *Qh = nullptr, *Qb = nullptr;      // query rows, as fp16 and as bf16: operands of the eight products along a row
+      float acc[16][4];          // [8 h + 2 m + e]: rows g8 and g8 + 8, dims d = 64 h + 8 c + 2 m + e of the columns c = 2 t4, 2 t4 + 1; times F 2^-24 (e = 0), F 2^-20 (e = 1)
+      float undo[2], l[2], zs[2][2], ref[2], over_by[2], F[2];      // per row, as in the other form; zs: [row][group]; F: [group]
+      // The share of a logit that does not come from codes, low_0 (sum of q over group 0) + low_1 (of group 1) - reference, is a product as well: bf16 planes of the three
+      // fp32 numbers of a query row (eight bits each, exact) against low_0 three times, low_1 three times, -1 three times.  This lane's part of the first operand:
+      uint32_t la[4];
+      float qsum[2][2];          // [row][group], log2 units
+      auto planes_of = [&](float y, uint32_t (&w)[3]) {      // bf16 bits of y = w0 + w1 + w2
+        uint32_t p[3];
+        split3_pair(y, 0.f, p);
+#pragma unroll
+        for (int i = 0; i < 3; ++i) w[i] = p[i] & 0xffffu;
+      };
+      auto set_rest = [&]() {
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          uint32_t p0[3], p1[3], pr[3];
+          planes_of(qsum[r][0], p0);
+          planes_of(qsum[r][1], p1);
+          planes_of(ref[r], pr);
+          // columns of the contraction: 0-2 q of group 0, 3-5 of group 1, 6-8 the reference; a lane has 2 t4, 2 t4 + 1 and 2 t4 + 8, 2 t4 + 9
+          la[r] = t4 == 0 ? p0[0] | p0[1] << 16 : (t4 == 1 ? p0[2] | p1[0] << 16 : (t4 == 2 ? p1[1] | p1[2] << 16 : pr[0] | pr[1] << 16));
+          la[2 + r] = t4 == 0 ? pr[2] : 0u;
+        }
+      };
+      // the other operand for the key that the two words are of: low_0 and low_1 in their upper halves
+      const uint32_t pick = t4 == 0 ? 0x3232u : (t4 == 1 ? 0x7632u : 0x7676u), minus_one = t4 == 0 ? 0xbf80u : 0u;
+      auto rest_of = [&](uint2 w) { return t4 == 3 ? 0xbf80bf80u : __byte_perm(w.x, w.y, pick); };
+      auto last_pos = [&](int r) { return a.causal ? progress[CW + 1] - a.T + (int)a.by_g.div((uint32_t)min(row0 + g8 + 8 * r, R - 1)) : 0x7fffffff; };
+
+      auto start = [&](int slot) {
+        Qh = reinterpret_cast<const uint4*>(smem + Shape::OFF_QH) + slot * 256 + lane;
+        Qb = reinterpret_cast<const uint4*>(smem + Shape::OFF_Q) + slot * 256 + lane;
+        const float* q_undo = reinterpret_cast<const float*>(smem + Shape::OFF_UNDO) + slot * 16;
+        F[0] = F[1] = 0x1p64f;
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const float off = q_undo[g8 + 8 * r] * sl2;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            float y = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const uint4 w = Qh[(4 * h + i) * 32];
+              const float2 e0 = f16_pair(r ? w.y : w.x), e1 = f16_pair(r ? w.w : w.z);
+              y += (e0.x + e0.y) + 16.f * (e1.x + e1.y);
+            }
+            y += __shfl_xor_sync(0xffffffffu, y, 1);
+            y += __shfl_xor_sync(0xffffffffu, y, 2);
+            qsum[r][h] = y * off;
+          }
+          undo[r] = off * 0x1p12f * 0x1p12f;
+          ref[r] = 0.f; over_by[r] = -INFINITY; l[r] = 0.f; zs[r][0] = zs[r][1] = 0.f;
+        }
+        set_rest();
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+#pragma unroll
+          for (int y = 0; y < 4; ++y) acc[i][y] = 0.f;
+      };
+
+      // logits minus reference to weights in place, [8 keys each][row g8: two keys; row g8 + 8: two keys]; s0, s1: the largest scales of this lane's keys
+      auto weigh = [&](auto& x, float s0, float s1) {
+        constexpr int N = (int)(sizeof(x) / sizeof(x[0]));
+        bool over = s0 * F[0] > 128.f || s1 * F[1] > 128.f;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+          for (int y = 0; y < 4; ++y) over |= x[i][y] > over_by[y >> 1];
+        if (__any_sync(0xffffffffu, over)) {
+          float most = 0.f;      // of the factors that the sums so far get
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            float top = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < N; ++i) top = fmaxf(top, fmaxf(x[i][2 * r], x[i][2 * r + 1]));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            const bool first = over_by[r] == -INFINITY;
+            const float to = ref[r] + (first ? (top == -INFINITY ? 0.f : top) : fmaxf(top, 0.f)), up = to - ref[r];
             const float f = first ? 1.f : ex2_fast(-up);
             most = fmaxf(most, f);
-            if (top != -INFINITY) over_by[nt][c] = QA_SLACK;
-            ref[nt][c] = to;
+            if (top != -INFINITY) over_by[r] = QA_SLACK;
+            ref[r] = to;
 #pragma unroll
-            for (int i = c; i < N; i += 2) x[nt][i] -= up;
-            l[nt][c] *= f;
+            for (int i = 0; i < N; ++i) { x[i][2 * r] -= up; x[i][2 * r + 1] -= up; }
+            l[r] *= f; zs[r][0] *= f; zs[r][1] *= f;
 #pragma unroll
-            for (int g = 0; g < NG; ++g) zs[nt][g][c] *= f;
-#pragma unroll
-            for (int m = 0; m < 8; ++m) { acc[nt][m][c] *= f; acc[nt][m][2 + c] *= f; }
+            for (int i = 0; i < 16; ++i) { acc[i][2 * r] *= f; acc[i][2 * r + 1] *= f; }
           }
-        most = warp_max(most);
+          most = warp_max(most);
 #pragma unroll
-        for (int g = 0; g < NG; ++g) {
-          float largest = g ? s1 : s0;      // of the group: DUO has the other one in the lanes t4 ^ 2
+          for (int h = 0; h < 2; ++h) {
+            const float largest = fmaxf(64.f / F[h] * most, warp_max(h ? s1 : s0));
+            const int e = min(max((int)(__float_as_uint(largest) >> 23) - 127, -58), 126);
+            const float to = __uint_as_float((uint32_t)(127 + 6 - e) << 23), f = to / F[h];
+            F[h] = to;
 #pragma unroll
-          for (int o = 16; o > 0; o >>= 1)
-            if (!DUO || o != 2) largest = fmaxf(largest, __shfl_xor_sync(0xffffffffu, largest, o));
-          largest = fmaxf(64.f / F[g] * most, largest);
-          const int e = min(max((int)(__float_as_uint(largest) >> 23) - 127, -58), 126);
-          const float to = __uint_as_float((uint32_t)(127 + 6 - e) << 23), f = to / F[g];
-          F[g] = to;
+            for (int i = 0; i < 8; ++i)
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int m = 0; m < (DUO ? 8 : 4); ++m)      // (DUO: what the lane holds of the other group's dims is nobody's)
-#pragma unroll
-              for (int y = 0; y < 4; ++y) acc[nt][4 * g + m][y] *= f;
+              for (int y = 0; y < 4; ++y) acc[8 * h + i][y] *= f;
+          }
+          set_rest();
         }
-      }
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+        for (int i = 0; i < N; ++i)
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          x[nt][i] = ex2_fast(x[nt][i]);
-          l[nt][i & 1] += x[nt][i];
-        }
-    };
+          for (int y = 0; y < 4; ++y) {
+            x[i][y] = ex2_fast(x[i][y]);
+            l[y >> 1] += x[i][y];
+          }
+      };
+      auto add_to = [](float (&sum)[4], const float (&d)[4], float by) {
+        const float2 f = make_float2(by, by);
+        const float2 p = fma2(make_float2(d[0], d[1]), f, make_float2(sum[0], sum[1])), q = fma2(make_float2(d[2], d[3]), f, make_float2(sum[2], sum[3]));
+        sum[0] = p.x; sum[1] = p.y; sum[2] = q.x; sum[3] = q.y;
+      };
 
-    auto add_to = [](float (&sum)[4], const float (&d)[4], float2 f01, float2 f23) {
-      const float2 p = fma2(make_float2(d[0], d[1]), f01, make_float2(sum[0], sum[1])), q = fma2(make_float2(d[2], d[3]), f23, make_float2(sum[2], sum[3]));
-      sum[0] = p.x; sum[1] = p.y; sum[2] = q.x; sum[3] = q.y;
-    };
-    // a tile of packed rows, UNITS times 16
-    auto packed_rows = [&](auto units, const unsigned char* base) {
-      constexpr int UNITS = decltype(units)::value;
-      float x[NT][4 * UNITS];
-      uint32_t va[UNITS][NG], vc[UNITS][NG];      // scale and lowest number of the rows g8 and g8 + 8, values
-      {
-        float d[UNITS][NT][2][4];      // two chains: the groups; DUO: even and odd words
-        uint4 ka[UNITS], kc[UNITS];
+      // 32 packed rows, or 16 (the end of a chunk that is not a multiple of 32: what lies in the second unit is of an earlier tile)
+      auto packed_rows = [&](int rows, const unsigned char* base) {
+        float x[4][4];             // [eight keys each]
+        {
+          float d[4][2][4];        // [eight keys][group]
 #pragma unroll
-        for (int u = 0; u < UNITS; ++u) {
-          ka[u] = *reinterpret_cast<const uint4*>(base + u * Q4_PAIR_BYTES + lane * 16);
-          kc[u] = *reinterpret_cast<const uint4*>(base + u * Q4_PAIR_BYTES + 512 + lane * 16);
-        }
+          for (int j = 0; j < 4; ++j) {
+            const uint4 q0 = Qh[2 * j * 32], q1 = Qh[(2 * j + 1) * 32];
+            const uint32_t A0[4] = {q0.x, q0.y, q0.z, q0.w}, A1[4] = {q1.x, q1.y, q1.z, q1.w};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          uint32_t pa[UNITS][4], pc[UNITS][4];
-#pragma unroll
-          for (int u = 0; u < UNITS; ++u) {
-            q4_spread(word_of(ka[u], j), pa[u]);
-            q4_spread(word_of(kc[u], j), pc[u]);
-          }
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            const uint4 qw = q_half(nt, j);
-#pragma unroll
-            for (int u = 0; u < UNITS; ++u) {
-              const uint32_t A0[4] = {pa[u][0], pc[u][0], pa[u][1], pc[u][1]}, A1[4] = {pa[u][2], pc[u][2], pa[u][3], pc[u][3]};
-              float(&to)[4] = d[u][nt][DUO ? j & 1 : j >> 1];
-              if (DUO ? j < 2 : (j & 1) == 0) mma_f16_first(to, A0, qw.x, qw.y);
-              else mma_f16_next(to, A0, qw.x, qw.y);
-              mma_f16_next(to, A1, qw.z, qw.w);
-            }
-          }
-        }
-        // x = low + s c: the sum over a group is s (what the MMAs give) + low (sum of q)
-#pragma unroll
-        for (int u = 0; u < UNITS; ++u) {
-          const unsigned char* kh = base + u * Q4_PAIR_BYTES + Q4_CODE_BYTES + g8 * 8;
-          const unsigned char* vh = kh + Q4_UNIT_BYTES;
-          if constexpr (DUO) {
-            // a lane has the sum of its own group; the other group's is in the lane t4 ^ 2
-            const int of = (t4 >> 1) * 4;
-            const uint32_t ha = *reinterpret_cast<const uint32_t*>(kh + of), hc = *reinterpret_cast<const uint32_t*>(kh + 64 + of);
-            const float sa = bf16lo(ha), sc = bf16lo(hc), la = bf16hi(ha), lc = bf16hi(hc);
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-              const float(&y)[2][4] = d[u][0];
-              const float half_ref = -0.5f * ref[0][c];
-              const float p = fmaf((y[0][c] + y[1][c]) * sa, undo[0][c], fmaf(la, qsum[0][0][c], half_ref));
-              const float q = fmaf((y[0][2 + c] + y[1][2 + c]) * sc, undo[0][c], fmaf(lc, qsum[0][0][c], half_ref));
-              x[0][4 * u + c] = p + __shfl_xor_sync(0xffffffffu, p, 2);
-              x[0][4 * u + 2 + c] = q + __shfl_xor_sync(0xffffffffu, q, 2);
-            }
-            va[u][0] = *reinterpret_cast<const uint32_t*>(vh + of);
-            vc[u][0] = *reinterpret_cast<const uint32_t*>(vh + 64 + of);
-          } else {
-            const uint2 ha = *reinterpret_cast<const uint2*>(kh), hc = *reinterpret_cast<const uint2*>(kh + 64), wa = *reinterpret_cast<const uint2*>(vh), wc = *reinterpret_cast<const uint2*>(vh + 64);
-            const float sa0 = bf16lo(ha.x), sa1 = bf16lo(ha.y), sc0 = bf16lo(hc.x), sc1 = bf16lo(hc.y);
-            const float la0 = bf16hi(ha.x), la1 = bf16hi(ha.y), lc0 = bf16hi(hc.x), lc1 = bf16hi(hc.y);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-              for (int c = 0; c < 2; ++c) {
-                const float(&y)[2][4] = d[u][nt];
-                x[nt][4 * u + c] = fmaf(fmaf(y[0][c], sa0, y[1][c] * sa1), undo[nt][c], fmaf(la0, qsum[nt][0][c], fmaf(la1, qsum[nt][NG - 1][c], -ref[nt][c])));
-                x[nt][4 * u + 2 + c] = fmaf(fmaf(y[0][2 + c], sc0, y[1][2 + c] * sc1), undo[nt][c], fmaf(lc0, qsum[nt][0][c], fmaf(lc1, qsum[nt][NG - 1][c], -ref[nt][c])));
-              }
-            va[u][0] = wa.x; va[u][NG - 1] = wa.y;
-            vc[u][0] = wc.x; vc[u][NG - 1] = wc.y;
-          }
-        }
-      }
-      float most[NG] = {};
-#pragma unroll
-      for (int u = 0; u < UNITS; ++u)
-#pragma unroll
-        for (int g = 0; g < NG; ++g) most[g] = fmaxf(most[g], fmaxf(bf16lo(va[u][g]), bf16lo(vc[u][g])));
-      weigh(x, most[0], most[NG - 1]);
-      uint32_t b[NG][UNITS][NT][2];      // weights times scale: MMA operands
-#pragma unroll
-      for (int g = 0; g < NG; ++g)
-#pragma unroll
-        for (int u = 0; u < UNITS; ++u) {
-          const float f_a = bf16lo(va[u][g]) * F[g], f_c = bf16lo(vc[u][g]) * F[g], l_a = bf16hi(va[u][g]), l_c = bf16hi(vc[u][g]);
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            const float* p = &x[nt][4 * u];
-            b[g][u][nt][0] = transpose_8x8(pack_f16x2(p[0] * f_a, p[1] * f_a));
-            b[g][u][nt][1] = transpose_8x8(pack_f16x2(p[2] * f_c, p[3] * f_c));
-#pragma unroll
-            for (int c = 0; c < 2; ++c) zs[nt][g][c] = fmaf(p[c], l_a, fmaf(p[2 + c], l_c, zs[nt][g][c]));
-          }
-        }
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int g = DUO ? 0 : h;
-        uint4 vw[UNITS];
-#pragma unroll
-        for (int u = 0; u < UNITS; ++u) vw[u] = *reinterpret_cast<const uint4*>(base + u * Q4_PAIR_BYTES + Q4_UNIT_BYTES + h * 512 + lane * 16);
-#pragma unroll
-        for (int m = 0; m < 4; ++m) {
-          float d[NT][4];
-#pragma unroll
-          for (int u = 0; u < UNITS; ++u) {
-            uint32_t A[4];
-            q4_spread(word_of(vw[u], m), A);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              if (u == 0) mma_f16_first(d[nt], A, b[g][u][nt][0], b[g][u][nt][1]);
-              else mma_f16_next(d[nt], A, b[g][u][nt][0], b[g][u][nt][1]);
+            for (int i = 0; i < 4; ++i) {
+              uint32_t b[4];
+              q4_spread(*reinterpret_cast<const uint32_t*>(base + (i >> 1) * Q4_PAIR_BYTES + (i & 1) * 512 + lane * 16 + 4 * j), b);
+              if ((j & 1) == 0) mma_f16_first(d[i][j >> 1], A0, b[0], b[1]);
+              else mma_f16_next(d[i][j >> 1], A0, b[0], b[1]);
+              mma_f16_next(d[i][j >> 1], A1, b[2], b[3]);
             }
           }
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) add_to(acc[nt][4 * h + m], d[nt], make_float2(1.f, 1.f), make_float2(1.f, 1.f));
-        }
-      }
-    };
-
-    // a tile of `rows` <= 8 bf16 rows, the first at position pos
-    auto bf16_rows = [&](int rows, int pos, const unsigned char* base) {
-      float x[NT][2];
-      {
-        float d[NT][2][4];
-        const uint4* kr = reinterpret_cast<const uint4*>(base + g8 * ROW_BYTES) + t4;
+          for (int i = 0; i < 4; ++i) {
+            const unsigned char* heads = base + (i >> 1) * Q4_PAIR_BYTES + Q4_CODE_BYTES + (i & 1) * 64;
+            const uint4 w = *reinterpret_cast<const uint4*>(heads + 16 * t4);      // the keys 2 t4 and 2 t4 + 1: scale and lowest number of both groups
+            const float s0a = bf16lo(w.x), s1a = bf16lo(w.y), s0b = bf16lo(w.z), s1b = bf16lo(w.w);
+            float rest[4];
+            mma_bf16_first(rest, la, rest_of(*reinterpret_cast<const uint2*>(heads + 8 * g8)), minus_one);
 #pragma unroll
-        for (int jw = 0; jw < 4; ++jw) {
-          const uint4 kw = kr[4 * jw];
-          const uint32_t A0[4] = {kw.x, 0u, kw.y, 0u}, A1[4] = {kw.z, 0u, kw.w, 0u};
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            const uint4 qw = *reinterpret_cast<const uint4*>(Qb + row_of(nt, g8) * D + 32 * jw + 8 * t4);
-            if ((jw & 1) == 0) mma_bf16_first(d[nt][jw >> 1], A0, qw.x, qw.y);
-            else mma_bf16_next(d[nt][jw >> 1], A0, qw.x, qw.y);
-            mma_bf16_next(d[nt][jw >> 1], A1, qw.z, qw.w);
+            for (int r = 0; r < 2; ++r) {
+              x[i][2 * r] = fmaf(fmaf(d[i][0][2 * r], s0a, d[i][1][2 * r] * s1a), undo[r], rest[2 * r]);
+              x[i][2 * r + 1] = fmaf(fmaf(d[i][0][2 * r + 1], s0b, d[i][1][2 * r + 1] * s1b), undo[r], rest[2 * r + 1]);
+            }
           }
         }
+        const bool whole = rows == QA_ROWS4;
+        if (!whole) {
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int c = 0; c < 2; ++c) x[nt][c] = fmaf(d[nt][0][c] + d[nt][1][c], sl2, -ref[nt][c]);
-        if (rows < QA_ROWS16 || a.causal) {
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int c = 0; c < 2; ++c)
-              if (g8 >= rows || pos + g8 > last_pos(nt, c)) x[nt][c] = -INFINITY;
+          for (int i = 2; i < 4; ++i) x[i][0] = x[i][1] = x[i][2] = x[i][3] = -INFINITY;
         }
-      }
-      uint4 e[2], o[2];      // this lane's numbers of the rows 2 t4 and 2 t4 + 1
+        uint4 vh[4];               // scale and lowest number of both groups of the keys 2 t4 and 2 t4 + 1, values
+        uint32_t most0 = 0u, most1 = 0u;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        e[h] = *reinterpret_cast<const uint4*>(base + QA_V_OFF + 2 * t4 * ROW_BYTES + h * 128 + g8 * 16);
-        o[h] = *reinterpret_cast<const uint4*>(base + QA_V_OFF + (2 * t4 + 1) * ROW_BYTES + h * 128 + g8 * 16);
-      }
-      if (rows < QA_ROWS16) {      // what an earlier tile left there may be anything
+        for (int i = 0; i < 4; ++i) {
+          vh[i] = *reinterpret_cast<const uint4*>(base + (i >> 1) * Q4_PAIR_BYTES + Q4_UNIT_BYTES + Q4_CODE_BYTES + (i & 1) * 64 + 16 * t4);
+          if (i >= 2 && !whole) vh[i] = make_uint4(0u, 0u, 0u, 0u);
+          most0 = max_bf16x2(most0, max_bf16x2(vh[i].x, vh[i].z));
+          most1 = max_bf16x2(most1, max_bf16x2(vh[i].y, vh[i].w));
+        }
+        weigh(x, bf16lo(most0), bf16lo(most1));
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          if (2 * t4 >= rows) e[h] = make_uint4(0u, 0u, 0u, 0u);
-          if (2 * t4 + 1 >= rows) o[h] = make_uint4(0u, 0u, 0u, 0u);
-        }
-      }
-      weigh(x, 0.f, 0.f);
-      // both planes of the weights in one MMA: rows 0-7 of its contraction have the first, rows 8-15, the same rows again, the second
-      uint32_t b[NT][2];
+          uint32_t A[2][4];        // weights times scale
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const uint32_t hi = pack_bf16x2(x[nt][0], x[nt][1]);
-        b[nt][0] = transpose_8x8(hi);
-        b[nt][1] = transpose_8x8(pack_bf16x2(x[nt][0] - bf16lo(hi), x[nt][1] - bf16hi(hi)));
-      }
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t wa = h ? vh[i].y : vh[i].x, wb = h ? vh[i].w : vh[i].z;
+            const float fa = bf16lo(wa) * F[h], fb = bf16lo(wb) * F[h], lo_a = bf16hi(wa), lo_b = bf16hi(wb);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const uint32_t ew[4] = {e[h].x, e[h].y, e[h].z, e[h].w}, ow[4] = {o[h].x, o[h].y, o[h].z, o[h].w};
-        const float f01 = F[DUO ? 0 : h] * 0x1p-24f, f23 = F[DUO ? 0 : h] * 0x1p-20f;
-#pragma unroll
-        for (int m = 0; m < 4; ++m) {
-          const uint32_t a0 = __byte_perm(ew[m], ow[m], 0x5410), a1 = __byte_perm(ew[m], ow[m], 0x7632);
-          const uint32_t A[4] = {a0, a1, a0, a1};
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            float d[4];
-            mma_bf16_first(d, A, b[nt][0], b[nt][1]);
-            add_to(acc[nt][4 * h + m], d, make_float2(f01, f01), make_float2(f23, f23));
-          }
-        }
-      }
-    };
-
-    // leaves the state of the sequence in shared memory
-    auto leave = [&]() {
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int c = 0; c < 2; ++c)
-#pragma unroll
-          for (int o = 4; o <= 16; o <<= 1) {
-            l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], o);
-#pragma unroll
-            for (int g = 0; g < NG; ++g) zs[nt][g][c] += __shfl_xor_sync(0xffffffffu, zs[nt][g][c], o);
-          }
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          float* st = states + (warp * COLS + row_of(nt, 2 * t4 + c)) * ATTN_PARTIAL_FLOATS;
-#pragma unroll
-          for (int g = 0; g < NG; ++g) {
-            const float zv = zs[nt][g][c], un = 1.f / F[g];
-            float* o = st + 64 * (DUO ? t4 >> 1 : g) + 8 * g8;
-            float y[8];
-#pragma unroll
-            for (int m = 0; m < 4; ++m) {
-              const float even = DUO && t4 >= 2 ? acc[nt][4 + m][c] : acc[nt][4 * g + m][c], odd = DUO && t4 >= 2 ? acc[nt][4 + m][2 + c] : acc[nt][4 * g + m][2 + c];
-              y[2 * m] = fmaf(even * 0x1p24f, un, zv);
-              y[2 * m + 1] = fmaf(odd * 0x1p20f, un, zv);
+            for (int r = 0; r < 2; ++r) {
+              A[i >> 1][2 * (i & 1) + r] = pack_f16x2(x[i][2 * r] * fa, x[i][2 * r + 1] * fb);
+              zs[r][h] = fmaf(x[i][2 * r], lo_a, fmaf(x[i][2 * r + 1], lo_b, zs[r][h]));
             }
-            *reinterpret_cast<float4*>(o) = make_float4(y[0], y[1], y[2], y[3]);
-            *reinterpret_cast<float4*>(o + 4) = make_float4(y[4], y[5], y[6], y[7]);
           }
-          if (g8 == 0 && (!DUO || t4 < 2)) { st[128] = over_by[nt][c] == -INFINITY ? -INFINITY : ref[nt][c]; st[129] = l[nt][c]; }
+          const uint4 v0 = *reinterpret_cast<const uint4*>(base + Q4_UNIT_BYTES + h * 512 + lane * 16), v1 = *reinterpret_cast<const uint4*>(base + Q4_PAIR_BYTES + Q4_UNIT_BYTES + h * 512 + lane * 16);
+#pragma unroll
+          for (int m = 0; m < 4; ++m) {
+            uint32_t b0[4], b1[4];
+            q4_spread(word_of(v0, m), b0);
+            q4_spread(word_of(v1, m), b1);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              float d[4];
+              mma_f16_first(d, A[0], b0[e], b0[2 + e]);
+              mma_f16_next(d, A[1], b1[e], b1[2 + e]);
+              add_to(acc[8 * h + 2 * m + e], d, 1.f);
+            }
+          }
         }
-      __syncwarp();
-    };
+      };
 
-    uint64_t *my_full = full + warp * STAGES, *my_empty = empty + warp * STAGES;
-    int nth = 0, stage = 0;      // sequences begun; stage of the next tile
-    uint32_t phase = 0;
-    bool ok = mbar_wait_bounded(fetched, 0);
-    if (!ok && lane == 0) set_status(v.status, ERR_TIMEOUT);
-    while (ok) {
-      if (!mbar_wait_bounded(&my_full[stage], phase)) {
-        if (lane == 0) set_status(v.status, ERR_TIMEOUT);
-        break;
-      }
-      const unsigned char* base = smem + (warp * STAGES + stage) * QA_TILE_BYTES;
-      const int4 what = infos[warp * STAGES + stage];
-      if (a.causal) n = progress[CW + 1];
-      if (what.y & QA_NEW) {      // its query rows were brought when the sequence two before it was merged, which this warp has waited for
-        start(nth & 1);
-        ++nth;
-      }
-      if (what.z == QA_ROWS4) packed_rows(std::integral_constant<int, 2>(), base);
-      else if (what.z > 0) packed_rows(std::integral_constant<int, 1>(), base);      // (the end of a chunk that is not a multiple of 32)
-      else if (what.z < 0) bf16_rows(-what.z, what.w, base);
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&my_empty[stage]);
-      if (what.y & QA_FLUSH) {
-        // the states of the sequence before are done with
-        if (nth >= 2 && !mbar_wait_bounded(merged, (uint32_t)(nth - 2) & 1u)) {
-          if (lane == 0) set_status(v.status, ERR_TIMEOUT);
-          break;
+      // `rows` <= 8 bf16 rows, the first at position pos
+      auto bf16_rows = [&](int rows, int pos, const unsigned char* base) {
+        float d[2][4], x[1][4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint4 q0 = Qb[2 * j * 32], q1 = Qb[(2 * j + 1) * 32];
+          const uint4 kw = *reinterpret_cast<const uint4*>(base + g8 * ROW_BYTES + 64 * j + 16 * t4);
+          const uint32_t A0[4] = {q0.x, q0.y, q0.z, q0.w}, A1[4] = {q1.x, q1.y, q1.z, q1.w};
+          if ((j & 1) == 0) mma_bf16_first(d[j >> 1], A0, kw.x, kw.y);
+          else mma_bf16_next(d[j >> 1], A0, kw.x, kw.y);
+          mma_bf16_next(d[j >> 1], A1, kw.z, kw.w);
         }
-        leave();
-        if (what.y & QA_END) break;
-        if (lane == 0) mbar_arrive(left);      // release
-      }
-      if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+#pragma unroll
+        for (int y = 0; y < 4; ++y) x[0][y] = fmaf(d[0][y] + d[1][y], sl2, -ref[y >> 1]);
+        if (rows < QA_ROWS16 || a.causal) {
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            const int key = 2 * t4 + (y & 1);
+            if (key >= rows || pos + key > last_pos(y >> 1)) x[0][y] = -INFINITY;
+          }
+        }
+        weigh(x, 0.f, 0.f);
+        // both planes of the weights in one product: rows 0-7 of its contraction have the first, rows 8-15, the same keys again, the second
+        uint32_t A[4];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          A[r] = pack_bf16x2(x[0][2 * r], x[0][2 * r + 1]);
+          A[2 + r] = pack_bf16x2(x[0][2 * r] - bf16lo(A[r]), x[0][2 * r + 1] - bf16hi(A[r]));
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint4 e = *reinterpret_cast<const uint4*>(base + QA_V_OFF + 2 * t4 * ROW_BYTES + h * 128 + g8 * 16), o = *reinterpret_cast<const uint4*>(base + QA_V_OFF + (2 * t4 + 1) * ROW_BYTES + h * 128 + g8 * 16);
+          if (2 * t4 >= rows) e = make_uint4(0u, 0u, 0u, 0u);      // what an earlier tile left there may be anything
+          if (2 * t4 + 1 >= rows) o = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+          for (int m = 0; m < 4; ++m)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+              const uint32_t b = __byte_perm(word_of(e, m), word_of(o, m), y ? 0x7632 : 0x5410);
+              float t[4];
+              mma_bf16_first(t, A, b, b);
+              add_to(acc[8 * h + 2 * m + y], t, F[h] * (y ? 0x1p-20f : 0x1p-24f));
+            }
+        }
+      };
+
+      auto leave = [&]() {
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+          for (int o = 1; o <= 2; o <<= 1) {
+            l[r] += __shfl_xor_sync(0xffffffffu, l[r], o);
+            zs[r][0] += __shfl_xor_sync(0xffffffffu, zs[r][0], o);
+            zs[r][1] += __shfl_xor_sync(0xffffffffu, zs[r][1], o);
+          }
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          float* st = states + (warp * COLS + g8 + 8 * r) * ATTN_PARTIAL_FLOATS;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const float un = 1.f / F[h];
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              float y[8];
+#pragma unroll
+              for (int i = 0; i < 8; ++i) y[i] = fmaf(acc[8 * h + i][2 * r + c] * (i & 1 ? 0x1p20f : 0x1p24f), un, zs[r][h]);
+              float* o = st + 64 * h + 8 * (2 * t4 + c);
+              *reinterpret_cast<float4*>(o) = make_float4(y[0], y[1], y[2], y[3]);
+              *reinterpret_cast<float4*>(o + 4) = make_float4(y[4], y[5], y[6], y[7]);
+            }
+          }
+          if (t4 == 0) { st[128] = over_by[r] == -INFINITY ? -INFINITY : ref[r]; st[129] = l[r]; }
+        }
+        __syncwarp();
+      };
+
+      consume(start, packed_rows, bf16_rows, leave);
     }
   }
 
@@ -839,7 +1131,7 @@ __global__ void __launch_bounds__(QaShape<NT, DUO>::WARPS * 32, 1) kve_decode_at
 }
 
 Q4AttnShape q4_attn_shape(int rows) {
-  const int cols = rows <= QaShape<1, true>::COLS ? QaShape<1, true>::COLS : (rows <= QaShape<1, false>::COLS ? QaShape<1, false>::COLS : QaShape<2, false>::COLS);
+  const int cols = rows <= 4 ? 4 : (rows <= 8 ? 8 : 16);
   return {cols, (rows + cols - 1) / cols};
 }
 
@@ -859,9 +1151,11 @@ cudaError_t launch_attn_q4(const LayerView& v, const Q4Pages& p, bool dense, int
     return e != cudaSuccess ? e : launch_pdl(kernel, dim3((unsigned)(runs * shape.groups)), dim3((unsigned)warps * 32), (size_t)smem, st, a);
   };
   static DeviceFlags f4, f8, f16;
-  if (shape.cols == QaShape<1, true>::COLS) return launch(kve_decode_attn_q4_kernel<1, true>, f4, QaShape<1, true>::WARPS, QaShape<1, true>::SMEM);
-  if (shape.cols == QaShape<1, false>::COLS) return launch(kve_decode_attn_q4_kernel<1, false>, f8, QaShape<1, false>::WARPS, QaShape<1, false>::SMEM);
-  return launch(kve_decode_attn_q4_kernel<2, false>, f16, QaShape<2, false>::WARPS, QaShape<2, false>::SMEM);
+  switch (shape.cols) {
+    case 4: return launch(kve_decode_attn_q4_kernel<4>, f4, QaShape<4>::WARPS, QaShape<4>::SMEM);
+    case 8: return launch(kve_decode_attn_q4_kernel<8>, f8, QaShape<8>::WARPS, QaShape<8>::SMEM);
+    default: return launch(kve_decode_attn_q4_kernel<16>, f16, QaShape<16>::WARPS, QaShape<16>::SMEM);
+  }
 }
 
 }  // namespace kve
