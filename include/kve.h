@@ -196,8 +196,8 @@ int kvE_gate_next(kvE_store* st, int layer, const kvE_lstm_weights* w, float tau
 int kvE_refresh_next(kvE_store* st, int layer, const kvE_agg_weights* aw, const kvE_lstm_weights* lw, float tau, void* stream);
 
 /* Read the stored length and the keep list's coverage of `layer` back from the device (waits for `stream`) and make them
- * the handle's: the token count, and - when the keep list covered every gated chunk before - the counts of summarised,
- * gated and listed chunks.  For use after replaying captured kvE_append_next / kvE_decode_step / kvE_refresh_next
+ * the handle's: the token count, the count of chunks held in 4 bits, and - when the keep list covered every gated chunk before - the counts of
+ * summarised, gated and listed chunks.  For use after replaying captured kvE_append_next / kvE_decode_step / kvE_refresh_next
  * launches, which move the device's counters without the host.  KVE_ERR_STATE if the device holds impossible values. */
 int kvE_adopt_device_state(kvE_store* st, int layer, void* stream);
 
@@ -318,7 +318,8 @@ int kvE_append_rope_next(kvE_store* st, int layer, const kvE_rows* q, const kvE_
  * c = count of the borders low + (k + 1/2) s, k = 0..14, that lie below x (on a border: the lower code); it stands for
  * low + c s.  Rows must be finite; a group that holds an infinity or a NaN stands for NaN throughout.
  * Chunks [0, n_packed) of a layer have such a copy (kvE_packed_chunks); n_packed is held on the device too.  kvE_set_len to a length that cuts
- * into them lowers it to the chunks that are still complete; a caller who writes pages himself sets the length to 0 first. */
+ * into them lowers it to the chunks that are still complete, on the device too when it is replayed; a caller who writes pages without these calls sets
+ * the length to 0 first. */
 #define KVE_Q4_UNIT_ROWS 16       /* C must be a multiple of it */
 #define KVE_Q4_UNIT_BYTES 2304    /* of 16 keys and 16 values: codes and scales */
 typedef struct {
@@ -339,7 +340,8 @@ int kvE_attach_q4(kvE_store* st, const kvE_q4_buffers* buf);
 
 /* Chunks [chunk_begin, chunk_end) of every sequence of `layer` to 4 bits, from their bf16 pages, which stay as they are
  * (kvE_reclaim_pages with KVE_RECLAIM_PACKED hands them back).  chunk_begin <= n_packed, chunk_end <= floor((n - W) / C): else
- * KVE_ERR_STATE.  Neither summaries nor scores are needed. */
+ * KVE_ERR_STATE.  KVE_ERR_GEOMETRY where S rows / 8 reaches 2^31 (take fewer chunks a call).  Neither summaries nor scores are needed.  Captured, a replay packs the same chunks again and
+ * leaves the device's n_packed at chunk_end or more, or where it was if chunks before chunk_begin are not packed then. */
 int kvE_pack_chunks(kvE_store* st, int layer, int chunk_begin, int chunk_end, void* stream);
 
 /* What chunks [chunk_begin, chunk_end) stand for, rounded to bf16: k_out, v_out DEVICE bf16 [S][(chunk_end - chunk_begin) C][d], on 16

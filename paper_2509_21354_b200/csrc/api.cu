@@ -412,11 +412,9 @@ int kvE_set_len(kvE_store* st, int layer, int n, void* stream) {
   LayerState& ls = st->layers[layer];
   const int nc = stale_chunks(st->cfg, n);
   // a keep list that reaches past the new stale range is dropped, on the device too (-1: leave the device's count alone)
-  // chunks that are no longer complete lose their 4-bit copy: other rows may take their place
-  const int complete = n / st->cfg.C, packed = ls.n_packed > complete ? complete : -1;
-  cudaError_t e = launch_set_len(view(st, layer), n, ls.n_compacted > nc ? 0 : -1, packed, static_cast<cudaStream_t>(stream));
+  cudaError_t e = launch_set_len(view(st, layer), n, ls.n_compacted > nc ? 0 : -1, static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return cuda_fail(st, e);
-  if (packed >= 0) ls.n_packed = packed;
+  if (ls.n_packed > n / st->cfg.C) ls.n_packed = n / st->cfg.C;      // (the kernel does the same to the device's count)
   ls.n_tokens = n;
   ls.reserve_upper = 0;
   if (ls.n_summarised > nc) ls.n_summarised = nc;
@@ -600,13 +598,15 @@ int kvE_adopt_device_state(kvE_store* st, int layer, void* stream) {
   LayerState& ls = st->layers[layer];
   const LayerView v = view(st, layer);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  int32_t len = 0, listed = 0;
+  int32_t len = 0, listed = 0, packed = 0;
   cudaError_t e = cudaMemcpyAsync(&len, v.seq_len, sizeof(len), cudaMemcpyDeviceToHost, s);
   if (e == cudaSuccess) e = cudaMemcpyAsync(&listed, v.n_listed, sizeof(listed), cudaMemcpyDeviceToHost, s);
+  if (e == cudaSuccess && v.n_packed) e = cudaMemcpyAsync(&packed, v.n_packed, sizeof(packed), cudaMemcpyDeviceToHost, s);
   if (e == cudaSuccess) e = cudaStreamSynchronize(s);
   if (e != cudaSuccess) return cuda_fail(st, e);
-  if (len < 0 || len > st->cfg.max_tokens || listed < 0 || listed > stale_chunks(st->cfg, len)) return KVE_ERR_STATE;
+  if (len < 0 || len > st->cfg.max_tokens || listed < 0 || listed > stale_chunks(st->cfg, len) || packed < 0) return KVE_ERR_STATE;
   ls.n_tokens = len;
+  ls.n_packed = packed < len / st->cfg.C ? packed : len / st->cfg.C;
   ls.reserve_upper = 0;
   if (ls.n_compacted > 0 && ls.n_compacted == ls.n_gated && ls.n_summarised == ls.n_gated && listed > 0)
     ls.n_summarised = ls.n_gated = ls.n_compacted = listed;      // triggers executed on the device move all three together
@@ -995,6 +995,9 @@ Q4Pages q4_pages(const kvE_store* st, int layer) {
                  st->q4.page_table4 + (size_t)layer * st->S * st->max_chunks};
 }
 
+// units of keys and of values in a call: the kernels count them in 32 bits
+bool too_many_units(const kvE_store* st, int chunks) { return 2LL * st->S * chunks * (st->cfg.C / Q4_UNIT_ROWS) > 0x7fffffffLL; }
+
 // How an attention launch is cut up: every sequence into k equal parts, `runs` CTAs (for every group of query rows) with a contiguous run of them each.
 // The cheaper of two ways, in microseconds: a number of CTAs of its own for every sequence, or one resident wave that goes from sequence to sequence, which costs
 // a CTA 3 us a turn (state to shared memory, another's query rows, a first tile that raises every reference) and 2.5 us where records meet.
@@ -1064,8 +1067,9 @@ int kvE_pack_chunks(kvE_store* st, int layer, int chunk_begin, int chunk_end, vo
   LayerState& ls = st->layers[layer];
   if (chunk_begin > ls.n_packed || chunk_end > stale_chunks(st->cfg, ls.n_tokens)) return KVE_ERR_STATE;
   if (chunk_end == chunk_begin) return KVE_OK;
+  if (too_many_units(st, chunk_end - chunk_begin)) return KVE_ERR_GEOMETRY;
   Prof prof(st, KVE_K_PACK, static_cast<cudaStream_t>(stream));
-  const cudaError_t e = launch_pack(view(st, layer), q4_pages(st, layer), chunk_begin, chunk_end, chunk_end > ls.n_packed ? chunk_end : -1, static_cast<cudaStream_t>(stream));
+  const cudaError_t e = launch_pack(view(st, layer), q4_pages(st, layer), chunk_begin, chunk_end, static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return cuda_fail(st, e);
   if (chunk_end > ls.n_packed) ls.n_packed = chunk_end;
   return KVE_OK;
@@ -1078,6 +1082,7 @@ int kvE_unpack_chunks(kvE_store* st, int layer, int chunk_begin, int chunk_end, 
   if (wrong_device(st) || !st->q4_ready) return KVE_ERR_STATE;
   if (chunk_end > st->layers[layer].n_packed) return KVE_ERR_STATE;
   if (chunk_end == chunk_begin) return KVE_OK;
+  if (too_many_units(st, chunk_end - chunk_begin)) return KVE_ERR_GEOMETRY;
   const cudaError_t e = launch_unpack(view(st, layer), q4_pages(st, layer), chunk_begin, chunk_end, k_out, v_out, static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? KVE_OK : cuda_fail(st, e);
 }

@@ -266,18 +266,14 @@ PyObject* unpack_chunks(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     const auto fn = reinterpret_cast<int (*)(void*, int, int, int, void*, void*, void*)>(PyLong_AsVoidPtr(a[0]));
     const int64_t S = x[3], rows = (int64_t)(x[2] > x[1] ? x[2] - x[1] : 0) * x[4];
     PyObject* out[2] = {a[9], a[10]};
-    void* p[2];
+    void* p[2] = {};
+    at::Tensor made[2];
     for (int i = 0; i < 2; ++i) {
       if (out[i] != Py_None) {
-        if (!shaped(out[i], at::kBFloat16, {S, rows, 128}, c.device, &p[i])) {
-          if (i) Py_DECREF(out[0]);
-          return nullptr;
-        }
-        Py_INCREF(out[i]);
+        if (!shaped(out[i], at::kBFloat16, {S, rows, 128}, c.device, &p[i])) return nullptr;
       } else {
-        at::Tensor t = at::empty({S, rows, 128}, at::TensorOptions().dtype(at::kBFloat16).device(at::kCUDA, (c10::DeviceIndex)c.device));
-        p[i] = t.data_ptr();
-        out[i] = THPVariable_Wrap(std::move(t));
+        made[i] = at::empty({S, rows, 128}, at::TensorOptions().dtype(at::kBFloat16).device(at::kCUDA, (c10::DeviceIndex)c.device));
+        p[i] = made[i].data_ptr();
       }
     }
     int rc = 0;
@@ -285,6 +281,10 @@ PyObject* unpack_chunks(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
       Py_BEGIN_ALLOW_THREADS
       rc = fn(c.handle, x[0], x[1], x[2], p[0], p[1], c.stream);
       Py_END_ALLOW_THREADS
+    }
+    for (int i = 0; i < 2; ++i) {
+      if (made[i].defined()) out[i] = THPVariable_Wrap(std::move(made[i]));
+      else Py_INCREF(out[i]);
     }
     return Py_BuildValue("(iNN)", rc, out[0], out[1]);
   } catch (const std::exception& e) {

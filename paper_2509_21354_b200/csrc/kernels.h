@@ -68,8 +68,8 @@ constexpr int ATTN_PARTIAL_FLOATS = 132;       // acc[128], m, l, 2 pad: keeps e
 // q_src, q_dst: S rows to copy along, or null
 cudaError_t launch_append(const LayerView& v, const void* k_new, const void* v_new, int n_new, int pos0, cudaStream_t st,
                           const void* q_src = nullptr, void* q_dst = nullptr);
-// n_listed >= 0: also set the device copy of the keep list's coverage to it; n_packed >= 0: that of the 4-bit chunks
-cudaError_t launch_set_len(const LayerView& v, int n, int n_listed, int n_packed, cudaStream_t st);
+// n_listed >= 0: also set the device copy of the keep list's coverage to it
+cudaError_t launch_set_len(const LayerView& v, int n, int n_listed, cudaStream_t st);
 cudaError_t launch_append_next(const LayerView& v, const void* k_new, const void* v_new, int n_new, int32_t* ticket,
                                cudaStream_t st);
 // q, k and v as they come: strides in elements over batch, token and head
@@ -93,7 +93,8 @@ struct Q4Pages {
   const int32_t* table;       // [S][max_chunks], this layer's
 };
 constexpr int Q4_UNIT_ROWS = 16, Q4_UNIT_BYTES = 1152, Q4_PAIR_BYTES = 2 * Q4_UNIT_BYTES;
-cudaError_t launch_pack(const LayerView& v, const Q4Pages& p, int t0, int t1, int n_packed, cudaStream_t st);
+// chunks [t0, t1); the device's count of packed chunks goes up to t1
+cudaError_t launch_pack(const LayerView& v, const Q4Pages& p, int t0, int t1, cudaStream_t st);
 cudaError_t launch_unpack(const LayerView& v, const Q4Pages& p, int t0, int t1, void* k_out, void* v_out, cudaStream_t st);
 // attention of T query tokens on G query heads a KV head.  Query rows go in `groups` of `cols`, one CTA each; every sequence is cut into parts_per_seq equal
 // parts, and `runs` CTAs per group share them; partials: (S + runs) groups records of `cols` rows of ATTN_PARTIAL_FLOATS; counters: S groups, zero between launches

@@ -8,10 +8,14 @@
 //    operand registers (fp16 numbers c 2^-24 and c 2^-20) in five logic instructions.  The powers of two go into q, into the softmax's scale and into
 //    the result; scale and lowest number of a group are applied to the sums (keys: per row and group to the logit) or to the weights (values:
 //    p s per group of 64 dims).  q enters as fp16 as well, times a power of two that puts its largest number at 2^14: exact but for numbers 2^25 below that.
-//  * both products are m16n8k16 MMAs with the cache on the M side (keys: 16 rows; values, transposed: 16 dims) and the queries in the
-//    eight columns.  The logits' accumulator becomes the weights' operand through movmatrix, in registers.
-//  * up to four query rows: the eight columns are the four rows twice, once for either group of 64 dims (q is zero in the other half; the weights have the
-//    group's scale), so that a lane has to do with one group only: half of the scales, weights and conversions.
+//  * all products are m16n8k16 MMAs.  Three forms, by the query rows of a CTA (q4_attn_shape), because the tensor core takes 16 rows by 8 columns whether they are used or not:
+//      1 to 4 rows: the cache on the M side (keys: 16 rows; values, transposed: 16 dims), the queries in the eight columns: the four rows twice, once for either group of 64
+//        dims (q is zero in the other half; the weights have the group's scale), so that a lane has to do with one group only: half of the scales, weights and conversions.
+//        16 sequences x 32 heads x 16512 rows, half of the chunks kept: 160 us; with the rows once in eight columns 170.
+//      5 to 8 rows: the same, a row a column.  128 sequences x 8320 rows: 43 us; with the queries on the M side 65.
+//        In both the logits' accumulator becomes the weights' operand through movmatrix, in registers.
+//      9 to 16 rows: the queries on the M side, where the logits' accumulator is the weights' operand as it stands.  The lowest numbers' share of a logit, minus the
+//        reference, is a product too, of three bf16 planes.  128 sequences x 8320 rows, 16 rows: 66 us; as two blocks of columns of the form above 72.
 //  * the weights p s F of packed rows are fp16: 11 bits, whose rounding (2^-12 a row) stays far below the result's own (2^-9).  F, a power of two per
 //    warp and group, follows the largest p s so that they neither overflow nor run out of bits.  bf16 rows take their weights as two bf16 planes.
 //  * a tile's products with the values are summed from zero and added to the accumulator by ordinary additions: the tensor core cuts off what lies below

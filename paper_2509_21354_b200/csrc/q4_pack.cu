@@ -51,12 +51,13 @@ __device__ __forceinline__ uint32_t q4_scale_bits(float high, float low) {
   return (u + 0x7fffu + ((u >> 16) & 1u)) >> 16;
 }
 
-// The codes of eight numbers of a group (c[i]: whole numbers 0..15).  TINY: scales may be so small that 1 / scale overflows: those are taken 2^64 times as large.
-template <bool TINY>
+// The codes of eight numbers of a group (c[i]: whole numbers 0..15).  ANY: scales may be so small that 1 / scale overflows, or so large that largest - low does: such
+// groups are taken times a power of two (exact: bf16 numbers keep 16 bits to spare at either end).
+template <bool ANY>
 __device__ __forceinline__ void q4_codes(const uint4& x, float scale, float low, float inv, float (&c)[8]) {
-  const float up = TINY && scale < 0x1p-60f ? 0x1p64f : 1.f;
-  const float s = TINY ? scale * up : scale, half = 0.5f * s;      // (scale 0: the codes do not matter)
-  if (TINY) inv = s > 0.f ? __frcp_rn(s) : 0.f;
+  const float up = !ANY ? 1.f : (scale < 0x1p-60f ? 0x1p64f : (scale > 0x1p120f ? 0x1p-8f : 1.f));
+  const float s = ANY ? scale * up : scale, half = 0.5f * s;      // (scale 0: the codes do not matter)
+  if (ANY) inv = s > 0.f ? __frcp_rn(s) : 0.f;
   const float2 up2 = make_float2(up, up), off = make_float2(-low * up, -low * up), inv2 = make_float2(inv, inv), neg_s = make_float2(-s, -s);
   const float2 eps = make_float2(-0x1p-12f, -0x1p-12f), magic = make_float2(0x1.8p23f, 0x1.8p23f), unmagic = make_float2(-0x1.8p23f, -0x1.8p23f);
   const uint32_t w[4] = {x.x, x.y, x.z, x.w};
@@ -76,12 +77,15 @@ __device__ __forceinline__ uint32_t q4_half(float c0, float c1, float c2, float 
   return __float_as_uint(fmaf(fmaf(c3, 16.f, c2), 256.f, fmaf(c1, 16.f, c0)) + 8388608.f);
 }
 
-__global__ void __launch_bounds__(PK_WARPS * 32) kve_pack_kernel(LayerView v, Q4Pages p, int t0, int n_chunks, int n_units, FastDiv by_units, FastDiv by_chunks, int n_packed) {
+__global__ void __launch_bounds__(PK_WARPS * 32) kve_pack_kernel(LayerView v, Q4Pages p, int t0, int n_chunks, int n_units, FastDiv by_units, FastDiv by_chunks) {
   __shared__ uint32_t codes[PK_WARPS][Q4_UNIT_ROWS * PK_PITCH];
   pdl_launch_dependents();
   pdl_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  if (blockIdx.x == 0 && threadIdx.x == 0 && n_packed >= 0) *v.n_packed = n_packed;
+  if (blockIdx.x == 0 && threadIdx.x == 0) {      // (a replay may find another length, or fewer chunks packed: none is named that has no rows, no gap left)
+    const int had = *v.n_packed, now = min(t0 + n_chunks, v.seq_len[0] / v.C);
+    if (had >= t0 && now > had) *v.n_packed = now;
+  }
   const int item = blockIdx.x * PK_WARPS + warp;
   if (item >= n_units) return;
   const int per_chunk = v.C / Q4_UNIT_ROWS;
@@ -119,14 +123,14 @@ __global__ void __launch_bounds__(PK_WARPS * 32) kve_pack_kernel(LayerView v, Q4
   const uint32_t sb = q4_scale_bits(bf16lo(m[0]), -bf16hi(m[0])), head = sb | (sb == 0x7fffu ? 0x7fff0000u : (m[0] & 0xffff0000u) ^ 0x80000000u);
   const float my_scale = __uint_as_float(sb << 16), my_inv = my_scale > 0.f ? __frcp_rn(my_scale) : 0.f;
   *reinterpret_cast<uint32_t*>(dst + Q4_CODE_BYTES + (2 * (lane & 7) + half) * 8 + ((lane >> 3) & 1) * 4) = head;
-  auto encode = [&](auto tiny) {
+  auto encode = [&](auto any) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int from = (lane & 24) | i, line = 2 * i + half;
       const uint32_t g = __shfl_sync(0xffffffffu, head, from);
       const float inv = __shfl_sync(0xffffffffu, my_inv, from);
       float c[8];
-      q4_codes<decltype(tiny)::value>(row[i], bf16lo(g), bf16hi(g), inv, c);
+      q4_codes<decltype(any)::value>(row[i], bf16lo(g), bf16hi(g), inv, c);
       if (is_v) {
         codes[warp][line * PK_PITCH + l16] = __byte_perm(q4_half(c[0], c[1], c[2], c[3]), q4_half(c[4], c[5], c[6], c[7]), 0x5410);
       } else {
@@ -135,7 +139,7 @@ __global__ void __launch_bounds__(PK_WARPS * 32) kve_pack_kernel(LayerView v, Q4
       }
     }
   };
-  if (__any_sync(0xffffffffu, my_scale > 0.f && my_scale < 0x1p-100f)) encode(std::true_type());
+  if (__any_sync(0xffffffffu, my_scale > 0.f && (my_scale < 0x1p-100f || my_scale > 0x1p120f))) encode(std::true_type());
   else encode(std::false_type());
   if (is_v) {
     __syncwarp();
@@ -213,11 +217,11 @@ static unsigned pack_grid(const LayerView& v, int chunks, int& n_units, FastDiv&
   return (unsigned)((n_units + PK_WARPS - 1) / PK_WARPS);
 }
 
-cudaError_t launch_pack(const LayerView& v, const Q4Pages& p, int t0, int t1, int n_packed, cudaStream_t st) {
+cudaError_t launch_pack(const LayerView& v, const Q4Pages& p, int t0, int t1, cudaStream_t st) {
   int n_units;
   FastDiv by_units, by_chunks;
   const unsigned grid = pack_grid(v, t1 - t0, n_units, by_units, by_chunks);
-  return launch_pdl(kve_pack_kernel, dim3(grid), dim3(PK_WARPS * 32), 0, st, v, p, t0, t1 - t0, n_units, by_units, by_chunks, n_packed);
+  return launch_pdl(kve_pack_kernel, dim3(grid), dim3(PK_WARPS * 32), 0, st, v, p, t0, t1 - t0, n_units, by_units, by_chunks);
 }
 
 cudaError_t launch_unpack(const LayerView& v, const Q4Pages& p, int t0, int t1, void* k_out, void* v_out, cudaStream_t st) {

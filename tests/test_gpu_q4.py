@@ -167,6 +167,27 @@ def test_pack_infinities_and_nan_stay_in_their_group():
         assert np.array_equal(nan, want)
 
 
+def test_pack_the_whole_range_of_bf16():
+    """groups whose numbers lie further apart than fp32 reaches, beside ordinary ones, and numbers of the smallest sizes there are"""
+    rng = np.random.default_rng(11)
+    x = rng.standard_normal((2, 128, 128)).astype(np.float32)
+    top = ref.number(np.uint16(0x7F7F))
+    x[0, ::2] = rng.uniform(-1, 1, size=(64, 128)) * top
+    x[0, 0, 3], x[0, 0, 4], x[0, 0, 64:] = top, -top, 1.0
+    x[0, 2, :64] = rng.integers(-15, 16, size=64) * np.exp2(123.0)         # on the borders
+    x[1, ::4] = np.exp2(rng.integers(-133, 128, size=(32, 128))) * rng.choice([-1.0, 1.0], size=(32, 128))
+    x[1, 1] *= np.exp2(-133.0)
+    K, V = ref.bits(x), ref.bits(x[::-1])
+    case = Case(Hkv=2, n=128, C_=64, W=0, K=from_bits(K), V=from_bits(V))
+    for got, rows in zip(case.st.unpack_chunks(0, 0, 2), (K, V)):
+        want, got = ref.quantise(rows)[0], numbers(got)
+        over = np.abs(want) >= 2.0 ** 128 * (1 - 2.0 ** -9)                # rounded to bf16 that is an infinity
+        assert np.array_equal(got[over], np.sign(want[over]) * np.inf)
+        # as above: 64 bits, fp32 rounding of the sum, one bf16 rounding
+        assert (np.abs(got - want)[~over] <= ((2.0 ** -8 + 2.0 ** -23) * np.abs(want) + 2.0 ** -134)[~over]).all()
+    assert case.st.poll_status() == 0
+
+
 def test_scale_is_rounded_once():
     """groups whose (largest - smallest) / 15 lies next to the middle of two bf16 numbers"""
     rng = np.random.default_rng(5)
@@ -347,6 +368,40 @@ def test_rolling_back_into_packed_chunks():
     case.check(dense=True)
     st.set_len(0, 0)
     assert st.packed_chunks(0) == 0
+
+
+def test_lengths_and_packing_replayed_on_another_state():
+    """a captured kvE_set_len lowers what the device holds packed at replay time; captured packing names no chunk without rows"""
+    case = Case(n=200, W=64, packed=0, max_tokens=740)
+    st = case.st
+    torch.cuda.synchronize()
+    cut, pack = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(cut):
+        st.set_len(0, 130)
+    st.adopt_device_state(0)
+    st.append(0, normal((2, 500, 128), 80), normal((2, 500, 128), 81))
+    st.pack_chunks(0, 0, 9)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(pack):
+        st.pack_chunks(0, 0, 9)
+    cut.replay()
+    st.adopt_device_state(0)
+    assert st.packed_chunks(0) == 2
+
+    def put(n, seed):
+        more = [normal((2, n, 128), seed + i) for i in range(2)]
+        st.append(0, *more)
+        case.K, case.V, case.n = torch.cat([case.K, more[0]], 1), torch.cat([case.V, more[1]], 1), case.n + n
+    case.K, case.V, case.n, case.packed = case.K[:, :130], case.V[:, :130], 130, 2
+    put(400, 82)
+    case.check(dense=True)
+    pack.replay()
+    st.adopt_device_state(0)
+    assert st.packed_chunks(0) == 8
+    case.packed = 8
+    case.check(dense=True)
+    put(100, 84)
+    case.check(dense=True)
 
 
 def test_layers_are_apart():
