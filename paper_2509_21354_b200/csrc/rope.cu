@@ -16,9 +16,9 @@
 namespace kve {
 
 constexpr int RP_THREADS = 256;
-constexpr int RP_CTAS = 6;                    // per SM (with four tokens each; 5 of them 273 us, 4 285)
+constexpr int RP_CTAS = 6;                    // per SM (8 x 4096 tokens of 96 rows: 258 us; 5 of them 273, 4 285)
 constexpr int RP_ROWS = RP_THREADS / 8;       // rows under way at a time
-constexpr int RP_MAX_TOKENS = 8;              // tokens of one CTA (few heads)
+constexpr int RP_MAX_TOKENS = 16;             // tokens of one CTA (few heads)
 constexpr int RP_TABLE = 8 * 9;               // (cos, sin) of pair 8 x + e at 9 x + e: eight threads read different banks
 
 struct RopeArgs : RopeCall {
@@ -168,10 +168,12 @@ cudaError_t launch_append_rope(const LayerView& v, const RopeCall& call, bool ne
   RopeArgs a;
   static_cast<RopeCall&>(a) = call;
   a.n_tokens = v.B * a.n_new;
-  // one pass of the CTA, or one token; with tokens for two full waves, up to four (the angles of four tokens take as long as those of one: 8 x 4096 tokens of
-  // 96 rows 396 us with one token a CTA, 301 with two, 269 with four, 276 with eight)
+  // one pass of the CTA, or one token; with tokens for two full waves, six passes (the rows of one pass are fetched while the ones before are turned and stored, and the
+  // angles of a few tokens take as long as those of one).  16 x 4096 tokens of 12 rows: 72 us, with one and a half passes 80; of 6 rows 48 and 65; of 9 rows 62 and 72;
+  // 8 x 4096 of 96 rows 258, with three passes 396, with twelve 261
   int per = RP_ROWS / rows, most = a.n_tokens / (2 * RP_CTAS * sm_count());
-  if (most > 4) most = 4;
+  const int want = (6 * RP_ROWS + rows - 1) / rows;
+  if (most > want) most = want;
   per = per < most ? most : per;
   per = per < 1 ? 1 : (per > RP_MAX_TOKENS ? RP_MAX_TOKENS : per);
   a.tokens_per_cta = per;

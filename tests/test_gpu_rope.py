@@ -98,6 +98,23 @@ def test_rope_append(B, Hkv, G, n0, n, sections, layout, fused, first, form):
             assert (x == 7.0).all()
 
 
+@pytest.mark.parametrize("Hkv,G,n", [(1, 1, 16600), (1, 7, 9100)])
+def test_many_tokens_of_few_heads(Hkv, G, n):
+    """as many tokens a CTA as there are"""
+    from paper_2509_21354_b200 import binding as b
+    st = store(2, Hkv, G, max_tokens=n + 3, page_perm="random", seed=5)
+    rope = b.Rope((40, 24))
+    q, k, v = projections(2, n, Hkv * G, Hkv, 6, True)
+    positions = np.random.default_rng(7).integers(0, 100000, size=(2, n, 2), dtype=np.int64)
+    out, _ = st.append_rope(0, q, k, v, rope, positions=torch.from_numpy(positions.astype(np.int32)).cuda())
+    torch.cuda.synchronize()
+    assert st.poll_status() == 0
+    check_turned(numbers(out), numbers(q), positions, rope)
+    got_k, got_v = stored(st, 0, n)
+    check_turned(got_k, numbers(k), positions, rope)
+    assert np.array_equal(got_v, numbers(v))
+
+
 @pytest.mark.parametrize("form", ["host", "device"])
 def test_positions_default_to_the_index_and_q_may_be_missing(form):
     from paper_2509_21354_b200 import binding as b
