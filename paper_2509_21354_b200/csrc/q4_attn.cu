@@ -215,6 +215,8 @@ __global__ void __launch_bounds__(QaShape<COLS>::WARPS * 32, 1) kve_decode_attn_
       if (piece == 0) q_undo[c] = __uint_as_float((uint32_t)(127 - power) << 23);
     }
   };
+  // one CTA has all parts of sequence x
+  auto whole = [&](int x) { return qa_owner((uint32_t)x * uk, n_items, P) == qa_owner((uint32_t)(x + 1) * uk - 1u, n_items, P); };
   // folds the consumers' states of query row r of sequence x: the result, or a record
   auto fold_states = [&](int x, int r) {
     const float* st = states + r * ATTN_PARTIAL_FLOATS;
@@ -224,7 +226,7 @@ __global__ void __launch_bounds__(QaShape<COLS>::WARPS * 32, 1) kve_decode_attn_
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int w = 0; w < CW; ++w) fold(st + w * COLS * ATTN_PARTIAL_FLOATS, top, sum, o, lane);
-    if (qa_owner((uint32_t)x * uk, n_items, P) == qa_owner((uint32_t)(x + 1) * uk - 1u, n_items, P)) {
+    if (whole(x)) {
       write_row(a, x, row0 + r, o, top, sum, lane);
     } else {
       float* rec = a.partials + (((long long)(x + run) * a.groups + group) * COLS + r) * ATTN_PARTIAL_FLOATS;
@@ -357,7 +359,7 @@ __global__ void __launch_bounds__(QaShape<COLS>::WARPS * 32, 1) kve_decode_attn_
       if (__any_sync(0xffffffffu, ready)) {
         idle = 0;
       } else {
-        __nanosleep(100);
+        if (pushed > 0) __nanosleep(100);
         if (++idle > (1 << 20)) {
           if (lane == 0) set_status(v.status, ERR_TIMEOUT);
           break;
@@ -1057,6 +1059,7 @@ __global__ void __launch_bounds__(QaShape<COLS>::WARPS * 32, 1) kve_decode_attn_
   // ---- the last sequence's states, by all warps; then sequences of which other CTAs have parts: the first and the last of this run ----
   __syncthreads();
   for (int r = warp; r < n_rows; r += WARPS) fold_states(x1, r);
+  if (whole(x0) && whole(x1)) return;
   __syncthreads();
   // The ticket is an acquire-release atomic at device scope, taken when all warps have written their records: it publishes them, and makes those of the other
   // CTAs visible to this one's warps once they have synchronised again.
