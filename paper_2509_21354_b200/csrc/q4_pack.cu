@@ -5,8 +5,8 @@
 // packed fp32 pairs.
 //
 // The codes are those of the real numbers, not of fp32 rounding: with bf16 input, numbers that lie on a border are not rare
-// (x - low and s have few bits: one number in 250 of a normal distribution).  rint((x - low) / s - 2^-12) is the code or one less, as the
-// quotient's own error is below 2^-18, and the remainder x - low - c s says which: x - low is rounded up, so that it is above a border
+// (x - low and s have few bits: one number in 250 of a normal distribution).  rint((x - low) / s (1 - 2^-13)) is the code or one less, as the
+// quotient's own relative error is below 2^-21 and it is 15 1/16 at most, and the remainder x - low - c s says which: x - low is rounded up, so that it is above a border
 // (which fp32 holds) exactly where the real difference is, and the remainder of that is exact.
 #include <type_traits>
 
@@ -15,6 +15,7 @@
 namespace kve {
 
 constexpr int PK_WARPS = 8;
+constexpr float PK_SHY = 1.f - 0x1p-13f;      // 1 / scale is taken that much smaller
 constexpr int PK_PITCH = 20;      // words of a row of values on their way between lanes: the four lanes of a column read different banks
 
 __device__ __forceinline__ uint32_t max2_nan(uint32_t a, uint32_t b) {
@@ -57,14 +58,14 @@ template <bool ANY>
 __device__ __forceinline__ void q4_codes(const uint4& x, float scale, float low, float inv, float (&c)[8]) {
   const float up = !ANY ? 1.f : (scale < 0x1p-60f ? 0x1p64f : (scale > 0x1p120f ? 0x1p-8f : 1.f));
   const float s = ANY ? scale * up : scale, half = 0.5f * s;      // (scale 0: the codes do not matter)
-  if (ANY) inv = s > 0.f ? __frcp_rn(s) : 0.f;
+  if (ANY) inv = s > 0.f ? __frcp_rn(s) * PK_SHY : 0.f;
   const float2 up2 = make_float2(up, up), off = make_float2(-low * up, -low * up), inv2 = make_float2(inv, inv), neg_s = make_float2(-s, -s);
-  const float2 eps = make_float2(-0x1p-12f, -0x1p-12f), magic = make_float2(0x1.8p23f, 0x1.8p23f), unmagic = make_float2(-0x1.8p23f, -0x1.8p23f);
+  const float2 magic = make_float2(0x1.8p23f, 0x1.8p23f), unmagic = make_float2(-0x1.8p23f, -0x1.8p23f);
   const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const float2 t = fma2_up(make_float2(bf16lo(w[e]), bf16hi(w[e])), up2, off);      // x - low
-    float2 n = add2(add2(fma2(t, inv2, eps), magic), unmagic);                        // the code, or one less
+    float2 n = add2(fma2(t, inv2, magic), unmagic);                                   // the code, or one less
     const float2 r = fma2(n, neg_s, t);
     if (r.x > half) n.x += 1.f;
     if (r.y > half) n.y += 1.f;
@@ -121,7 +122,7 @@ __global__ void __launch_bounds__(PK_WARPS * 32) kve_pack_kernel(LayerView v, Q4
     }
   }
   const uint32_t sb = q4_scale_bits(bf16lo(m[0]), -bf16hi(m[0])), head = sb | (sb == 0x7fffu ? 0x7fff0000u : (m[0] & 0xffff0000u) ^ 0x80000000u);
-  const float my_scale = __uint_as_float(sb << 16), my_inv = my_scale > 0.f ? __frcp_rn(my_scale) : 0.f;
+  const float my_scale = __uint_as_float(sb << 16), my_inv = my_scale > 0.f ? __frcp_rn(my_scale) * PK_SHY : 0.f;
   *reinterpret_cast<uint32_t*>(dst + Q4_CODE_BYTES + (2 * (lane & 7) + half) * 8 + ((lane >> 3) & 1) * 4) = head;
   auto encode = [&](auto any) {
 #pragma unroll
