@@ -404,6 +404,50 @@ def test_lengths_and_packing_replayed_on_another_state():
     case.check(dense=True)
 
 
+def test_pages_whose_offsets_pass_32_bits():
+    from paper_2509_21354_b200 import binding as b
+    chunks, C_, n, G = 16600, 1024, 2100, 2                # numbers and 4-bit bytes of the pool both pass 2^31
+    far = np.arange(chunks, dtype=np.int32)[::-1]
+    st = b.Store(B=1, H=1, Hq=G, C_=C_, W=20, max_tokens=chunks * C_, d_g=64, page_perm=far)
+    st.attach_q4(page_perm=far)
+    q, k, v = normal((1, n, G, 128), 1), normal((1, n, 1, 128), 2), normal((1, n, 1, 128), 3)
+    turned, _ = st.append_rope(0, q, k, v, b.Rope((0, 64)), positions=torch.zeros((1, n, 2), dtype=torch.int32, device="cuda"))      # (an angle of 0)
+    assert torch.equal(turned, q)
+    st.pack_chunks(0, 0, 2)
+    K, V = as_bits(k)[0, :, 0], as_bits(v)[0, :, 0]
+    kq, vq = ref.quantise(K[:2048])[0], ref.quantise(V[:2048])[0]
+    for got, want in zip(st.unpack_chunks(0, 0, 2), (kq, vq)):
+        assert (np.abs(numbers(got)[0] - want) <= (2.0 ** -8 + 2.0 ** -23) * np.abs(want) + 2.0 ** -134).all()
+    out = st.decode_attn_q4(0, q[:, -1:].contiguous(), dense=True)
+    assert st.poll_status() == 0
+    want, _, spread = ref.attend(numbers(q)[0, -1], np.concatenate([kq, ref.number(K[2048:])]), np.concatenate([vq, ref.number(V[2048:])]), np.ones((G, n), bool))
+    assert (np.abs(numbers(out)[0, 0] - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -13 * spread).all()      # (Case.compare's bound with logits of this size)
+
+
+def test_two_graphs_of_one_handle_in_turn():
+    """launches of different shapes share the records and counters of the workspace"""
+    case = Case(B=2, Hkv=3, G=4, n=1500, T=5)
+    st = case.st
+    calls = []
+    for T, causal in ((1, False), (5, True), (3, False)):
+        q = normal((2, T, 12, 128), 60 + T)
+        out, lse = torch.empty_like(q), torch.empty(q.shape[:3], dtype=torch.float32, device="cuda")
+        run = lambda q=q, out=out, lse=lse, causal=causal: st.decode_attn_q4(0, q, dense=True, causal=causal, out=out, lse=lse)
+        run()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            run()
+        calls.append((graph, out, lse, out.clone(), lse.clone(), q))      # (q: the graph reads it)
+    for i in (0, 1, 2, 1, 0, 2, 2, 0):
+        calls[i][1].fill_(7.0)
+        calls[i][0].replay()
+    torch.cuda.synchronize()
+    assert st.poll_status() == 0
+    for _, out, lse, want, want_lse, _ in calls:
+        assert torch.equal(out, want) and torch.equal(lse, want_lse)
+
+
 def test_layers_are_apart():
     case = Case(n=500, n_layers=3, layer=1, Hkv=2)
     st = case.st
