@@ -1001,8 +1001,8 @@ bool too_many_units(const kvE_store* st, int chunks) { return 2LL * st->S * chun
 // How an attention launch is cut up: every sequence into k equal parts, `runs` CTAs (for every group of query rows) with a contiguous run of them each.
 // The cheaper of two ways, in microseconds: a number of CTAs of its own for every sequence, or one resident wave that goes from sequence to sequence, which costs
 // a CTA 3 us a turn (state to shared memory, another's query rows, a first tile that raises every reference) and 2.5 us where records meet.
-// Measured (graph of launches): 8 sequences of 100003 rows, 4 query rows: 16 CTAs each 34.4 us, 148 CTAs in a wave 35.7, 8 each 52.8; 64 of 4099: 2 each 19.7, wave 22.3 to
-// 26.8; 128 of 4167, half kept: 1 each 19.4, wave 23.7; 512 of 16512, half kept: wave of halves 170, of fifths 178, of whole sequences 191.
+// Measured (graph of launches): 8 sequences of 100003 rows, 4 query rows: 16 CTAs each 30.8 us, 8 each 52.8; 64 of 4099: 2 each 18.4, wave 24.3; 128 of 4167, half kept:
+// 1 each 17.4, wave of halves 23.0; 512 of 16512, half kept: wave of halves 156, of fifths 162, of whole sequences 173, 1 each after another 181.
 struct Q4Cut { int k, runs; };
 Q4Cut q4_cut(const kvE_store* st, const LayerState& ls, bool dense, int rows) {
   const int C = st->cfg.C;

@@ -16,7 +16,7 @@
 namespace kve {
 
 constexpr int RP_THREADS = 256;
-constexpr int RP_CTAS = 6;                    // per SM (8 x 4096 tokens of 96 rows: 258 us; 5 of them 273, 4 285)
+constexpr int RP_CTAS = 6;                    // per SM (8 x 4096 tokens of 96 rows: 258 us; 5 of them 264, 4 281, 8 301)
 constexpr int RP_ROWS = RP_THREADS / 8;       // rows under way at a time
 constexpr int RP_MAX_TOKENS = 16;             // tokens of one CTA (few heads)
 constexpr int RP_TABLE = 8 * 9;               // (cos, sin) of pair 8 x + e at 9 x + e: eight threads read different banks
