@@ -7,7 +7,7 @@
 //
 // HBM-bound: (Hq + 2 Hkv) rows of 256 bytes a token are read and written once.  All heads of a token share its 64 angles, so a CTA
 // takes whole tokens: its first threads work out the angles while the first rows are on their way, the rest is one pass.  A thread holds
-// the 16 numbers of eight pairs of one row (two 16-byte pieces, 64 numbers apart or side by side), eight threads a row.
+// 16 numbers of one row (two 16-byte pieces, 64 numbers apart), whose pairs it has whole in either layout; eight threads a row.
 #include <type_traits>
 
 #include "common.cuh"
@@ -16,7 +16,7 @@
 namespace kve {
 
 constexpr int RP_THREADS = 256;
-constexpr int RP_CTAS = 6;                    // per SM (8 x 4096 tokens of 96 rows: 258 us; 5 of them 264, 4 281, 8 301)
+constexpr int RP_CTAS = 6;                    // per SM (8 x 4096 tokens of 96 rows: 254 us; 5 of them 264, 4 281, 8 301)
 constexpr int RP_ROWS = RP_THREADS / 8;       // rows under way at a time
 constexpr int RP_MAX_TOKENS = 16;             // tokens of one CTA (few heads)
 constexpr int RP_TABLE = 8 * 9;               // (cos, sin) of pair 8 x + e at 9 x + e: eight threads read different banks
@@ -36,7 +36,7 @@ __global__ void __launch_bounds__(RP_THREADS, RP_CTAS) kve_append_rope_kernel(La
   const int tid = threadIdx.x, x = tid & 7;
   const int tok0 = blockIdx.x * a.tokens_per_cta, n_tok = min(a.tokens_per_cta, a.n_tokens - tok0);
   const int rows = a.Hq + 2 * v.H, n_items = n_tok * rows;
-  const int off_a = a.adjacent ? 16 * x : 8 * x, off_b = a.adjacent ? 16 * x + 8 : 64 + 8 * x;      // the thread's two pieces of a row
+  const int off_a = 8 * x, off_b = 64 + 8 * x;      // the thread's two pieces of a row (adjacent pairs too: side by side they made half of every 32-byte sector a load of its own, 257 -> 265 us)
 
   // a row under way: its numbers, its token, where it goes (null: nowhere), whether it turns
   struct Row { uint4 lo, hi; uint16_t* dst; int tok; bool turns; };
@@ -117,12 +117,12 @@ __global__ void __launch_bounds__(RP_THREADS, RP_CTAS) kve_append_rope_kernel(La
     if (cur.dst != nullptr) {
       uint4 lo = cur.lo, hi = cur.hi;
       if (cur.turns) {
-        const float2* cs = table[cur.tok] + x * 9;
+        const float2* cs = table[cur.tok] + (a.adjacent ? (x >> 1) * 9 + (x & 1) * 4 : x * 9);      // of pairs 8 x .. 8 x + 7; adjacent: of 4 x .. + 3, those of the second piece 32 pairs on
         uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
         if (a.adjacent) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const float2 f = cs[e];
+            const float2 f = cs[e < 4 ? e : 4 * 9 + e - 4];
             const float p = bf16lo(w[e]), q = bf16hi(w[e]);
             w[e] = pack_bf16x2(p * f.x - q * f.y, q * f.x + p * f.y);
           }
@@ -170,7 +170,7 @@ cudaError_t launch_append_rope(const LayerView& v, const RopeCall& call, bool ne
   a.n_tokens = v.B * a.n_new;
   // one pass of the CTA, or one token; with tokens for two full waves, six passes (the rows of one pass are fetched while the ones before are turned and stored, and the
   // angles of a few tokens take as long as those of one).  16 x 4096 tokens of 12 rows: 72 us, with one and a half passes 80; of 6 rows 48 and 65; of 9 rows 62 and 72;
-  // 8 x 4096 of 96 rows 258, with three passes 396, with twelve 261
+  // 8 x 4096 of 96 rows 254, with three passes 396, with twelve 261
   int per = RP_ROWS / rows, most = a.n_tokens / (2 * RP_CTAS * sm_count());
   const int want = (6 * RP_ROWS + rows - 1) / rows;
   if (most > want) most = want;
