@@ -17,7 +17,7 @@
 //      9 to 16 rows: the queries on the M side, where the logits' accumulator is the weights' operand as it stands.  The lowest numbers' share of a logit, minus the
 //        reference, is a product too, of three bf16 planes.  128 sequences x 8320 rows, 16 rows: 66 us; as two blocks of columns of the form above 72.
 //  * the weights p s F of packed rows are fp16: 11 bits, whose rounding (2^-12 a row) stays far below the result's own (2^-9).  F, a power of two per
-//    warp and group, follows the largest p s so that they neither overflow nor run out of bits.  bf16 rows take their weights as two bf16 planes.
+//    warp, query row and group, keeps them between what fp16 overflows at and where it runs out of bits (qa_factor).  bf16 rows take their weights as two bf16 planes.
 //  * a tile's products with the values are summed from zero and added to the accumulator by ordinary additions: the tensor core cuts off what lies below
 //    the last bit of its accumulator at every step, always in one direction.
 //  * the reference of the softmax is raised only when a logit passes it by more than 2^8 (a vote), not at every tile.
@@ -40,6 +40,8 @@ constexpr int QA_V_OFF = 2 * Q4_UNIT_BYTES;                  // bf16 rows: value
 constexpr int QA_ROWS4 = 2 * Q4_UNIT_ROWS, QA_ROWS16 = 8;    // rows of a tile of either kind
 static_assert(QA_ROWS16 * ROW_BYTES <= QA_V_OFF, "eight bf16 rows fit a stage");
 constexpr float QA_SLACK = 8.f;                              // by how much (log2) a logit may pass the softmax reference
+constexpr float QA_TOP = 128.f;                              // most that scale times factor may be: with weights of up to 2^QA_SLACK their product stays below fp16's 2^16
+constexpr int QA_F_MOST = 64;                                // exponent of the largest factor, and of the first
 constexpr int QA_PLAN = 128;                                 // tiles looked up ahead of the copies
 constexpr int QA_NEW = 1 << 16, QA_FLUSH = 2 << 16, QA_END = 4 << 16;          // first, last tile of a sequence for this warp; nothing comes after it
 
@@ -69,7 +71,8 @@ template <int COLS_> struct QaShape {
   static constexpr int OFF_Q = OFF_STATE + CW * COLS * ATTN_PARTIAL_FLOATS * 4;          // [2][query rows][128] bf16; the same as fp16; what undoes their powers of two: [2][query rows]
   static constexpr int OFF_QH = OFF_Q + 2 * COLS * ROW_BYTES;
   static constexpr int OFF_UNDO = OFF_QH + 2 * QROWS * ROW_BYTES;
-  static constexpr int OFF_INFO = OFF_UNDO + 2 * COLS * 4;   // [consumers][stages] int4: the tile's entry of the table
+  static constexpr int OFF_SUMS = OFF_UNDO + 2 * COLS * 4;   // MANY: sums of the query rows over the groups, times scale: [2][query rows][2]
+  static constexpr int OFF_INFO = OFF_SUMS + (MANY ? 2 * COLS * 8 : 0);      // [consumers][stages] int4: the tile's entry of the table
   static constexpr int OFF_PLAN = OFF_INFO + CW * STAGES * 16;      // [QA_PLAN] int4: tiles looked up
   static constexpr int OFF_BAR = OFF_PLAN + QA_PLAN * 16;
   static constexpr int SMEM = OFF_BAR + (2 * CW * STAGES + 3) * 8 + 16 + (CW + 2) * 4;
@@ -119,6 +122,17 @@ __device__ __forceinline__ void fold(const float* st, float top, float& sum, flo
   const float4 x = *reinterpret_cast<const float4*>(st + lane * 4);
   sum = fmaf(st[129], f, sum);
   o.x = fmaf(x.x, f, o.x); o.y = fmaf(x.y, f, o.y); o.z = fmaf(x.z, f, o.z); o.w = fmaf(x.w, f, o.w);
+}
+// The power of two that a query row's fp16 weights of a group are taken times, from now on.  now: its exponent so far; raw: the largest scale in the tile; most: the largest
+// weight times scale so far; f: what a raised reference leaves of earlier weights.  Scales like the tile's are to fit with a weight of 2^QA_SLACK (to 2^7), so that rows like
+// these do not ask again.  But a scale whose row has next to no weight must not take the bits of the others: `most` keeps 2^-3, whose fp16 numbers are normal down to 2^-11
+// of it.  (The tile's own weights fit either way; a tile with a scale beyond 2^7 over the factor asks again.)  Without a raised reference the factor only sinks.
+__device__ __forceinline__ int qa_exponent(float x) { return (int)((__float_as_uint(x) >> 23) & 255u) - 127; }      // 2^e <= x; 0: -127; not finite: 128
+__device__ __forceinline__ float qa_power(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
+__device__ __forceinline__ int qa_factor(int now, float raw, float most, float f) {
+  const int er = qa_exponent(raw), fit = max(6 - er, -3 - qa_exponent(most));
+  const int up = min(now - qa_exponent(f), now + 100);
+  return max(min(min(up, QA_F_MOST), min(fit, 125 - er)), -118);      // (scale times factor stays finite)
 }
 // a warp writes query row rr of sequence s
 __device__ __forceinline__ void write_row(const Q4AttnArgs& a, int s, int rr, float4 o, float top, float sum, int lane) {
@@ -440,15 +454,14 @@ __global__ void __launch_bounds__(QaShape<COLS>::WARPS * 32, 1) kve_decode_attn_
       float l[NT][2], zs[NT][NG][2]; // this lane's rows' share, per column: sum of weights; of weights times what code 0 stands for
       // per column: the softmax's reference (0 until there is one), and what a logit may exceed it by (-inf until there is one)
       float ref[NT][2], over_by[NT][2];
-      float F[NG];     // weight factor of a group: the largest p s so far times F lies in [2^6, 2^7); a scale with s F > 2^7 asks for another
-        // (2^64 at most, and to begin with: sums of bf16 rows times F stay finite below |v| = 2^60)
+      float F[NG][2];  // weight factors of the columns; a scale with s F > 2^7 asks for another (2^64 at most, and to begin with: sums of bf16 rows times F stay finite below |v| = 2^60)
+      // the largest weight times scale that column c has had in a tile that was looked at (in what the records do not use of the state, for the rare case alone)
+      auto most_of = [&](int nt, int g, int c) { return states + (warp * COLS + row_of(nt, 2 * t4 + c)) * ATTN_PARTIAL_FLOATS + 130 + (DUO ? t4 >> 1 : g); };
       // a fresh state, and the query rows in slot `slot`
       auto start = [&](int slot) {
         Qh = reinterpret_cast<const uint16_t*>(smem + Shape::OFF_QH) + slot * Shape::QROWS * D;
         Qb = reinterpret_cast<const uint16_t*>(smem + Shape::OFF_Q) + slot * COLS * D;
         const float* q_undo = reinterpret_cast<const float*>(smem + Shape::OFF_UNDO) + slot * COLS;
-#pragma unroll
-        for (int g = 0; g < NG; ++g) F[g] = 0x1p64f;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           float sum[NG] = {};
@@ -473,7 +486,7 @@ __global__ void __launch_bounds__(QaShape<COLS>::WARPS * 32, 1) kve_decode_attn_
             undo[nt][c] = q_undo[row_of(nt, 2 * t4 + c)] * 0x1p12f * sl2 * 0x1p12f;
             ref[nt][c] = 0.f; over_by[nt][c] = -INFINITY; l[nt][c] = 0.f;
 #pragma unroll
-            for (int g = 0; g < NG; ++g) zs[nt][g][c] = 0.f;
+            for (int g = 0; g < NG; ++g) { zs[nt][g][c] = 0.f; F[g][c] = qa_power(QA_F_MOST); }
           }
 #pragma unroll
           for (int m = 0; m < 8; ++m)
@@ -483,18 +496,24 @@ __global__ void __launch_bounds__(QaShape<COLS>::WARPS * 32, 1) kve_decode_attn_
       };
 
       // Logits minus reference (log2 units; of each of this lane's rows: c, c + 1) to weights in place.  s: the largest scale of
-      // these rows in either group.  Raises reference and factors where it has to.
-      auto weigh = [&](auto& x, float s0, float s1) {
+      // these rows in either group; scale(row, group): theirs one by one.  Raises the reference and changes the factors where it has to.
+      auto weigh = [&](auto& x, float s0, float s1, auto&& scale) {
         constexpr int N = (int)(sizeof(x[0]) / sizeof(float));
         bool over = false;
 #pragma unroll
-        for (int g = 0; g < NG; ++g) over |= (g ? s1 : s0) * F[g] > 128.f;
+        for (int g = 0; g < NG; ++g) over |= (g ? s1 : s0) * fmaxf(F[g][0], F[g][1]) > QA_TOP;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int i = 0; i < N; ++i) over |= x[nt][i] > over_by[nt][i & 1];
         if (__any_sync(0xffffffffu, over)) {
-          float most = 0.f;      // of the factors that the sums so far get
+          float raw[NG];
+#pragma unroll
+          for (int g = 0; g < NG; ++g) {
+            raw[g] = g ? s1 : s0;
+#pragma unroll
+            for (int o = 4; o <= 16; o <<= 1) raw[g] = fmaxf(raw[g], __shfl_xor_sync(0xffffffffu, raw[g], o));
+          }
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -507,35 +526,33 @@ __global__ void __launch_bounds__(QaShape<COLS>::WARPS * 32, 1) kve_decode_attn_
               const bool first = over_by[nt][c] == -INFINITY;
               const float to = ref[nt][c] + (first ? (top == -INFINITY ? 0.f : top) : fmaxf(top, 0.f)), up = to - ref[nt][c];
               const float f = first ? 1.f : ex2_fast(-up);
-              most = fmaxf(most, f);
               if (top != -INFINITY) over_by[nt][c] = QA_SLACK;
               ref[nt][c] = to;
 #pragma unroll
               for (int i = c; i < N; i += 2) x[nt][i] -= up;
               l[nt][c] *= f;
 #pragma unroll
-              for (int g = 0; g < NG; ++g) zs[nt][g][c] *= f;
-#pragma unroll
               for (int m = 0; m < 8; ++m) { acc[nt][m][c] *= f; acc[nt][m][2 + c] *= f; }
+#pragma unroll
+              for (int g = 0; g < NG; ++g) {
+                zs[nt][g][c] *= f;
+                float ps = 0.f;      // the tile's largest weight times scale
+#pragma unroll
+                for (int i = c; i < N; i += 2) ps = fmaxf(ps, ex2_fast(x[nt][i]) * scale(i >> 1, g));
+#pragma unroll
+                for (int o = 4; o <= 16; o <<= 1) ps = fmaxf(ps, __shfl_xor_sync(0xffffffffu, ps, o));
+                float* at = most_of(nt, g, c);
+                const float most = first ? ps : fmaxf(*at * f, ps);
+                const int was = qa_exponent(F[g][c]), now = qa_factor(was, raw[g], most, f);
+                const float by = qa_power(max(now - was, -127));
+                __syncwarp();
+                *at = most;      // (the lanes of a column write the same)
+                F[g][c] = qa_power(now);
+#pragma unroll
+                for (int m = 0; m < (DUO ? 8 : 4); ++m) { acc[nt][4 * g + m][c] *= by; acc[nt][4 * g + m][2 + c] *= by; }      // (DUO: what the lane holds of the other group's dims is nobody's)
+              }
             }
-          most = warp_max(most);
-#pragma unroll
-          for (int g = 0; g < NG; ++g) {
-            float largest = g ? s1 : s0;      // of the group: DUO has the other one in the lanes t4 ^ 2
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1)
-              if (!DUO || o != 2) largest = fmaxf(largest, __shfl_xor_sync(0xffffffffu, largest, o));
-            largest = fmaxf(64.f / F[g] * most, largest);
-            const int e = min(max((int)(__float_as_uint(largest) >> 23) - 127, -58), 126);
-            const float to = __uint_as_float((uint32_t)(127 + 6 - e) << 23), f = to / F[g];
-            F[g] = to;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-              for (int m = 0; m < (DUO ? 8 : 4); ++m)      // (DUO: what the lane holds of the other group's dims is nobody's)
-#pragma unroll
-                for (int y = 0; y < 4; ++y) acc[nt][4 * g + m][y] *= f;
-          }
+          __syncwarp();
         }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -627,18 +644,21 @@ __global__ void __launch_bounds__(QaShape<COLS>::WARPS * 32, 1) kve_decode_attn_
         for (int u = 0; u < UNITS; ++u)
 #pragma unroll
           for (int g = 0; g < NG; ++g) most[g] = fmaxf(most[g], fmaxf(bf16lo(va[u][g]), bf16lo(vc[u][g])));
-        weigh(x, most[0], most[NG - 1]);
+        weigh(x, most[0], most[NG - 1], [&](int row, int g) { return bf16lo(row & 1 ? vc[row >> 1][g] : va[row >> 1][g]); });
         uint32_t b[NG][UNITS][NT][2];      // weights times scale: MMA operands
 #pragma unroll
         for (int g = 0; g < NG; ++g)
 #pragma unroll
           for (int u = 0; u < UNITS; ++u) {
-            const float f_a = bf16lo(va[u][g]) * F[g], f_c = bf16lo(vc[u][g]) * F[g], l_a = bf16hi(va[u][g]), l_c = bf16hi(vc[u][g]);
+            const float s_a = bf16lo(va[u][g]), s_c = bf16lo(vc[u][g]);
+            const float2 F2 = make_float2(F[g][0], F[g][1]), f_a = mul2(make_float2(s_a, s_a), F2), f_c = mul2(make_float2(s_c, s_c), F2);
+            const float l_a = bf16hi(va[u][g]), l_c = bf16hi(vc[u][g]);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
               const float* p = &x[nt][4 * u];
-              b[g][u][nt][0] = transpose_8x8(pack_f16x2(p[0] * f_a, p[1] * f_a));
-              b[g][u][nt][1] = transpose_8x8(pack_f16x2(p[2] * f_c, p[3] * f_c));
+              const float2 w_a = mul2(make_float2(p[0], p[1]), f_a), w_c = mul2(make_float2(p[2], p[3]), f_c);
+              b[g][u][nt][0] = transpose_8x8(pack_f16x2(w_a.x, w_a.y));
+              b[g][u][nt][1] = transpose_8x8(pack_f16x2(w_c.x, w_c.y));
 #pragma unroll
               for (int c = 0; c < 2; ++c) zs[nt][g][c] = fmaf(p[c], l_a, fmaf(p[2 + c], l_c, zs[nt][g][c]));
             }
@@ -711,7 +731,7 @@ __global__ void __launch_bounds__(QaShape<COLS>::WARPS * 32, 1) kve_decode_attn_
             if (2 * t4 + 1 >= rows) o[h] = make_uint4(0u, 0u, 0u, 0u);
           }
         }
-        weigh(x, 0.f, 0.f);
+        weigh(x, 0.f, 0.f, [](int, int) { return 0.f; });
         // both planes of the weights in one MMA: rows 0-7 of its contraction have the first, rows 8-15, the same rows again, the second
         uint32_t b[NT][2];
 #pragma unroll
@@ -723,7 +743,8 @@ __global__ void __launch_bounds__(QaShape<COLS>::WARPS * 32, 1) kve_decode_attn_
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const uint32_t ew[4] = {e[h].x, e[h].y, e[h].z, e[h].w}, ow[4] = {o[h].x, o[h].y, o[h].z, o[h].w};
-          const float f01 = F[DUO ? 0 : h] * 0x1p-24f, f23 = F[DUO ? 0 : h] * 0x1p-20f;
+          const float(&f)[2] = F[DUO ? 0 : h];
+          const float2 f01 = make_float2(f[0] * 0x1p-24f, f[1] * 0x1p-24f), f23 = make_float2(f[0] * 0x1p-20f, f[1] * 0x1p-20f);
 #pragma unroll
           for (int m = 0; m < 4; ++m) {
             const uint32_t a0 = __byte_perm(ew[m], ow[m], 0x5410), a1 = __byte_perm(ew[m], ow[m], 0x7632);
@@ -732,7 +753,7 @@ __global__ void __launch_bounds__(QaShape<COLS>::WARPS * 32, 1) kve_decode_attn_
             for (int nt = 0; nt < NT; ++nt) {
               float d[4];
               mma_bf16_first(d, A, b[nt][0], b[nt][1]);
-              add_to(acc[nt][4 * h + m], d, make_float2(f01, f01), make_float2(f23, f23));
+              add_to(acc[nt][4 * h + m], d, f01, f23);
             }
           }
         }
@@ -757,7 +778,7 @@ __global__ void __launch_bounds__(QaShape<COLS>::WARPS * 32, 1) kve_decode_attn_
             float* st = states + (warp * COLS + row_of(nt, 2 * t4 + c)) * ATTN_PARTIAL_FLOATS;
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
-              const float zv = zs[nt][g][c], un = 1.f / F[g];
+              const float zv = zs[nt][g][c], un = 1.f / F[g][c];
               float* o = st + 64 * (DUO ? t4 >> 1 : g) + 8 * g8;
               float y[8];
 #pragma unroll
@@ -783,11 +804,13 @@ __global__ void __launch_bounds__(QaShape<COLS>::WARPS * 32, 1) kve_decode_attn_
       // query rows g8 and g8 + 8 and two keys of every eight ----
       const uint4 *Qh = nullptr, *Qb = nullptr;      // query rows, as fp16 and as bf16: operands of the eight products along a row
       float acc[16][4];          // [8 h + 2 m + e]: rows g8 and g8 + 8, dims d = 64 h + 8 c + 2 m + e of the columns c = 2 t4, 2 t4 + 1; times F 2^-24 (e = 0), F 2^-20 (e = 1)
-      float undo[2], l[2], zs[2][2], ref[2], over_by[2], F[2];      // per row, as in the other form; zs: [row][group]; F: [group]
+      float undo[2], l[2], zs[2][2], ref[2], over_by[2];      // per row, as in the other form; zs: [row][group]
+      uint32_t F[2];             // [group]: the factors of both rows, as bf16
+      auto most_of = [&](int r, int h) { return states + (warp * COLS + g8 + 8 * r) * ATTN_PARTIAL_FLOATS + 130 + h; };
       // The share of a logit that does not come from codes, low_0 (sum of q over group 0) + low_1 (of group 1) - reference, is a product as well: bf16 planes of the three
       // fp32 numbers of a query row (eight bits each, exact) against low_0 three times, low_1 three times, -1 three times.  This lane's part of the first operand:
       uint32_t la[4];
-      float qsum[2][2];          // [row][group], log2 units
+      float* qsum = nullptr;     // of the rows in use: [row][group], log2 units (used in the rare case only; all warps write the same)
       auto planes_of = [&](float y, uint32_t (&w)[3]) {      // bf16 bits of y = w0 + w1 + w2
         uint32_t p[3];
         split3_pair(y, 0.f, p);
@@ -798,8 +821,8 @@ __global__ void __launch_bounds__(QaShape<COLS>::WARPS * 32, 1) kve_decode_attn_
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
           uint32_t p0[3], p1[3], pr[3];
-          planes_of(qsum[r][0], p0);
-          planes_of(qsum[r][1], p1);
+          planes_of(qsum[2 * (g8 + 8 * r)], p0);
+          planes_of(qsum[2 * (g8 + 8 * r) + 1], p1);
           planes_of(ref[r], pr);
           // columns of the contraction: 0-2 q of group 0, 3-5 of group 1, 6-8 the reference; a lane has 2 t4, 2 t4 + 1 and 2 t4 + 8, 2 t4 + 9
           la[r] = t4 == 0 ? p0[0] | p0[1] << 16 : (t4 == 1 ? p0[2] | p1[0] << 16 : (t4 == 2 ? p1[1] | p1[2] << 16 : pr[0] | pr[1] << 16));
@@ -815,7 +838,7 @@ __global__ void __launch_bounds__(QaShape<COLS>::WARPS * 32, 1) kve_decode_attn_
         Qh = reinterpret_cast<const uint4*>(smem + Shape::OFF_QH) + slot * 256 + lane;
         Qb = reinterpret_cast<const uint4*>(smem + Shape::OFF_Q) + slot * 256 + lane;
         const float* q_undo = reinterpret_cast<const float*>(smem + Shape::OFF_UNDO) + slot * 16;
-        F[0] = F[1] = 0x1p64f;
+        qsum = reinterpret_cast<float*>(smem + Shape::OFF_SUMS) + slot * 32;
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
           const float off = q_undo[g8 + 8 * r] * sl2;
@@ -830,7 +853,8 @@ __global__ void __launch_bounds__(QaShape<COLS>::WARPS * 32, 1) kve_decode_attn_
             }
             y += __shfl_xor_sync(0xffffffffu, y, 1);
             y += __shfl_xor_sync(0xffffffffu, y, 2);
-            qsum[r][h] = y * off;
+            qsum[2 * (g8 + 8 * r) + h] = y * off;
+            F[h] = (uint32_t)(127 + QA_F_MOST) * 0x00800080u;
           }
           undo[r] = off * 0x1p12f * 0x1p12f;
           ref[r] = 0.f; over_by[r] = -INFINITY; l[r] = 0.f; zs[r][0] = zs[r][1] = 0.f;
@@ -842,16 +866,22 @@ __global__ void __launch_bounds__(QaShape<COLS>::WARPS * 32, 1) kve_decode_attn_
           for (int y = 0; y < 4; ++y) acc[i][y] = 0.f;
       };
 
-      // logits minus reference to weights in place, [8 keys each][row g8: two keys; row g8 + 8: two keys]; s0, s1: the largest scales of this lane's keys
-      auto weigh = [&](auto& x, float s0, float s1) {
+      // logits minus reference to weights in place, [8 keys each][row g8: two keys; row g8 + 8: two keys]; s0, s1: the largest scales of this lane's keys;
+      // scale(i, k, group): that of key k of the i-th eight
+      auto weigh = [&](auto& x, float s0, float s1, auto&& scale) {
         constexpr int N = (int)(sizeof(x) / sizeof(x[0]));
-        bool over = s0 * F[0] > 128.f || s1 * F[1] > 128.f;
+        bool over = s0 * fmaxf(bf16lo(F[0]), bf16hi(F[0])) > QA_TOP || s1 * fmaxf(bf16lo(F[1]), bf16hi(F[1])) > QA_TOP;
 #pragma unroll
         for (int i = 0; i < N; ++i)
 #pragma unroll
           for (int y = 0; y < 4; ++y) over |= x[i][y] > over_by[y >> 1];
         if (__any_sync(0xffffffffu, over)) {
-          float most = 0.f;      // of the factors that the sums so far get
+          float raw[2] = {s0, s1};
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            raw[h] = fmaxf(raw[h], __shfl_xor_sync(0xffffffffu, raw[h], 1));
+            raw[h] = fmaxf(raw[h], __shfl_xor_sync(0xffffffffu, raw[h], 2));
+          }
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
             float top = -INFINITY;
@@ -862,7 +892,6 @@ __global__ void __launch_bounds__(QaShape<COLS>::WARPS * 32, 1) kve_decode_attn_
             const bool first = over_by[r] == -INFINITY;
             const float to = ref[r] + (first ? (top == -INFINITY ? 0.f : top) : fmaxf(top, 0.f)), up = to - ref[r];
             const float f = first ? 1.f : ex2_fast(-up);
-            most = fmaxf(most, f);
             if (top != -INFINITY) over_by[r] = QA_SLACK;
             ref[r] = to;
 #pragma unroll
@@ -870,19 +899,25 @@ __global__ void __launch_bounds__(QaShape<COLS>::WARPS * 32, 1) kve_decode_attn_
             l[r] *= f; zs[r][0] *= f; zs[r][1] *= f;
 #pragma unroll
             for (int i = 0; i < 16; ++i) { acc[i][2 * r] *= f; acc[i][2 * r + 1] *= f; }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              float ps = 0.f;      // the tile's largest weight times scale
+#pragma unroll
+              for (int i = 0; i < N; ++i) ps = fmaxf(ps, fmaxf(ex2_fast(x[i][2 * r]) * scale(i, 0, h), ex2_fast(x[i][2 * r + 1]) * scale(i, 1, h)));
+              ps = fmaxf(ps, __shfl_xor_sync(0xffffffffu, ps, 1));
+              ps = fmaxf(ps, __shfl_xor_sync(0xffffffffu, ps, 2));
+              float* at = most_of(r, h);
+              const float most = first ? ps : fmaxf(*at * f, ps);
+              const int was = qa_exponent(r ? bf16hi(F[h]) : bf16lo(F[h])), now = qa_factor(was, raw[h], most, f);
+              const float by = qa_power(max(now - was, -127));
+              __syncwarp();
+              *at = most;      // (the lanes of a row write the same)
+              F[h] = __byte_perm(F[h], __float_as_uint(qa_power(now)), r ? 0x7610 : 0x3276);
+#pragma unroll
+              for (int i = 0; i < 8; ++i) { acc[8 * h + i][2 * r] *= by; acc[8 * h + i][2 * r + 1] *= by; }
+            }
           }
-          most = warp_max(most);
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const float largest = fmaxf(64.f / F[h] * most, warp_max(h ? s1 : s0));
-            const int e = min(max((int)(__float_as_uint(largest) >> 23) - 127, -58), 126);
-            const float to = __uint_as_float((uint32_t)(127 + 6 - e) << 23), f = to / F[h];
-            F[h] = to;
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-#pragma unroll
-              for (int y = 0; y < 4; ++y) acc[8 * h + i][y] *= f;
-          }
+          __syncwarp();
           set_rest();
         }
 #pragma unroll
@@ -893,9 +928,8 @@ __global__ void __launch_bounds__(QaShape<COLS>::WARPS * 32, 1) kve_decode_attn_
             l[y >> 1] += x[i][y];
           }
       };
-      auto add_to = [](float (&sum)[4], const float (&d)[4], float by) {
-        const float2 f = make_float2(by, by);
-        const float2 p = fma2(make_float2(d[0], d[1]), f, make_float2(sum[0], sum[1])), q = fma2(make_float2(d[2], d[3]), f, make_float2(sum[2], sum[3]));
+      auto add_to = [](float (&sum)[4], const float (&d)[4], float by0, float by1) {      // times the factors of the rows g8 and g8 + 8
+        const float2 p = fma2(make_float2(d[0], d[1]), make_float2(by0, by0), make_float2(sum[0], sum[1])), q = fma2(make_float2(d[2], d[3]), make_float2(by1, by1), make_float2(sum[2], sum[3]));
         sum[0] = p.x; sum[1] = p.y; sum[2] = q.x; sum[3] = q.y;
       };
 
@@ -945,17 +979,17 @@ __global__ void __launch_bounds__(QaShape<COLS>::WARPS * 32, 1) kve_decode_attn_
           most0 = max_bf16x2(most0, max_bf16x2(vh[i].x, vh[i].z));
           most1 = max_bf16x2(most1, max_bf16x2(vh[i].y, vh[i].w));
         }
-        weigh(x, bf16lo(most0), bf16lo(most1));
+        weigh(x, bf16lo(most0), bf16lo(most1), [&](int i, int k, int h) { return bf16lo(k ? (h ? vh[i].w : vh[i].z) : (h ? vh[i].y : vh[i].x)); });
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           uint32_t A[2][4];        // weights times scale
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const uint32_t wa = h ? vh[i].y : vh[i].x, wb = h ? vh[i].w : vh[i].z;
-            const float fa = bf16lo(wa) * F[h], fb = bf16lo(wb) * F[h], lo_a = bf16hi(wa), lo_b = bf16hi(wb);
+            const float sa = bf16lo(wa), sb = bf16lo(wb), lo_a = bf16hi(wa), lo_b = bf16hi(wb);
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
-              A[i >> 1][2 * (i & 1) + r] = pack_f16x2(x[i][2 * r] * fa, x[i][2 * r + 1] * fb);
+              A[i >> 1][2 * (i & 1) + r] = pack_f16x2(x[i][2 * r] * (sa * (r ? bf16hi(F[h]) : bf16lo(F[h]))), x[i][2 * r + 1] * (sb * (r ? bf16hi(F[h]) : bf16lo(F[h]))));
               zs[r][h] = fmaf(x[i][2 * r], lo_a, fmaf(x[i][2 * r + 1], lo_b, zs[r][h]));
             }
           }
@@ -970,7 +1004,7 @@ __global__ void __launch_bounds__(QaShape<COLS>::WARPS * 32, 1) kve_decode_attn_
               float d[4];
               mma_f16_first(d, A[0], b0[e], b0[2 + e]);
               mma_f16_next(d, A[1], b1[e], b1[2 + e]);
-              add_to(acc[8 * h + 2 * m + e], d, 1.f);
+              add_to(acc[8 * h + 2 * m + e], d, 1.f, 1.f);
             }
           }
         }
@@ -997,7 +1031,7 @@ __global__ void __launch_bounds__(QaShape<COLS>::WARPS * 32, 1) kve_decode_attn_
             if (key >= rows || pos + key > last_pos(y >> 1)) x[0][y] = -INFINITY;
           }
         }
-        weigh(x, 0.f, 0.f);
+        weigh(x, 0.f, 0.f, [](int, int, int) { return 0.f; });
         // both planes of the weights in one product: rows 0-7 of its contraction have the first, rows 8-15, the same keys again, the second
         uint32_t A[4];
 #pragma unroll
@@ -1017,7 +1051,7 @@ __global__ void __launch_bounds__(QaShape<COLS>::WARPS * 32, 1) kve_decode_attn_
               const uint32_t b = __byte_perm(word_of(e, m), word_of(o, m), y ? 0x7632 : 0x5410);
               float t[4];
               mma_bf16_first(t, A, b, b);
-              add_to(acc[8 * h + 2 * m + y], t, F[h] * (y ? 0x1p-20f : 0x1p-24f));
+              add_to(acc[8 * h + 2 * m + y], t, bf16lo(F[h]) * (y ? 0x1p-20f : 0x1p-24f), bf16hi(F[h]) * (y ? 0x1p-20f : 0x1p-24f));
             }
         }
       };
@@ -1036,7 +1070,7 @@ __global__ void __launch_bounds__(QaShape<COLS>::WARPS * 32, 1) kve_decode_attn_
           float* st = states + (warp * COLS + g8 + 8 * r) * ATTN_PARTIAL_FLOATS;
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const float un = 1.f / F[h];
+            const float un = 1.f / (r ? bf16hi(F[h]) : bf16lo(F[h]));
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
               float y[8];
