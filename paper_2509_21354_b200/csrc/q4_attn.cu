@@ -41,7 +41,7 @@ constexpr int QA_ROWS4 = 2 * Q4_UNIT_ROWS, QA_ROWS16 = 8;    // rows of a tile o
 static_assert(QA_ROWS16 * ROW_BYTES <= QA_V_OFF, "eight bf16 rows fit a stage");
 constexpr float QA_SLACK = 8.f;                              // by how much (log2) a logit may pass the softmax reference
 constexpr float QA_TOP = 128.f;                              // most that scale times factor may be: with weights of up to 2^QA_SLACK their product stays below fp16's 2^16
-constexpr int QA_F_MOST = 64;                                // exponent of the largest factor, and of the first
+constexpr int QA_F_MOST = 56;                                // exponent of the largest factor, and of the first: sums of 2^23 bf16 rows of |v| = 2^60, at weights of 2^QA_SLACK, stay finite times F 2^-20
 constexpr int QA_PLAN = 128;                                 // tiles looked up ahead of the copies
 constexpr int QA_NEW = 1 << 16, QA_FLUSH = 2 << 16, QA_END = 4 << 16;          // first, last tile of a sequence for this warp; nothing comes after it
 
@@ -454,7 +454,7 @@ __global__ void __launch_bounds__(QaShape<COLS>::WARPS * 32, 1) kve_decode_attn_
       float l[NT][2], zs[NT][NG][2]; // this lane's rows' share, per column: sum of weights; of weights times what code 0 stands for
       // per column: the softmax's reference (0 until there is one), and what a logit may exceed it by (-inf until there is one)
       float ref[NT][2], over_by[NT][2];
-      float F[NG][2];  // weight factors of the columns; a scale with s F > 2^7 asks for another (2^64 at most, and to begin with: sums of bf16 rows times F stay finite below |v| = 2^60)
+      float F[NG][2];  // weight factors of the columns; a scale with s F > 2^7 asks for another
       // the largest weight times scale that column c has had in a tile that was looked at (in what the records do not use of the state, for the rare case alone)
       auto most_of = [&](int nt, int g, int c) { return states + (warp * COLS + row_of(nt, 2 * t4 + c)) * ATTN_PARTIAL_FLOATS + 130 + (DUO ? t4 >> 1 : g); };
       // a fresh state, and the query rows in slot `slot`
@@ -784,8 +784,8 @@ __global__ void __launch_bounds__(QaShape<COLS>::WARPS * 32, 1) kve_decode_attn_
 #pragma unroll
               for (int m = 0; m < 4; ++m) {
                 const float even = DUO && t4 >= 2 ? acc[nt][4 + m][c] : acc[nt][4 * g + m][c], odd = DUO && t4 >= 2 ? acc[nt][4 + m][2 + c] : acc[nt][4 * g + m][2 + c];
-                y[2 * m] = fmaf(even * 0x1p24f, un, zv);
-                y[2 * m + 1] = fmaf(odd * 0x1p20f, un, zv);
+                y[2 * m] = fmaf(even * un, 0x1p24f, zv);      // (in this order: sums of large values times 2^24 may pass what fp32 holds)
+                y[2 * m + 1] = fmaf(odd * un, 0x1p20f, zv);
               }
               *reinterpret_cast<float4*>(o) = make_float4(y[0], y[1], y[2], y[3]);
               *reinterpret_cast<float4*>(o + 4) = make_float4(y[4], y[5], y[6], y[7]);
@@ -1075,7 +1075,7 @@ __global__ void __launch_bounds__(QaShape<COLS>::WARPS * 32, 1) kve_decode_attn_
             for (int c = 0; c < 2; ++c) {
               float y[8];
 #pragma unroll
-              for (int i = 0; i < 8; ++i) y[i] = fmaf(acc[8 * h + i][2 * r + c] * (i & 1 ? 0x1p20f : 0x1p24f), un, zs[r][h]);
+              for (int i = 0; i < 8; ++i) y[i] = fmaf(acc[8 * h + i][2 * r + c] * un, i & 1 ? 0x1p20f : 0x1p24f, zs[r][h]);
               float* o = st + 64 * h + 8 * (2 * t4 + c);
               *reinterpret_cast<float4*>(o) = make_float4(y[0], y[1], y[2], y[3]);
               *reinterpret_cast<float4*>(o + 4) = make_float4(y[4], y[5], y[6], y[7]);

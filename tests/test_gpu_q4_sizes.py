@@ -1,5 +1,5 @@
 """Attention over 4 bits with values of very different sizes in one sequence, against the 64-bit restatement: rows much larger than the rest
-whose weight is next to nothing and query rows that disagree about which rows matter."""
+whose weight is next to nothing, query rows that disagree about which rows matter, sums next to the end of the declared range."""
 import numpy as np
 import pytest
 import torch
@@ -136,3 +136,19 @@ def test_weights_that_rise_along_the_sequence(G):
         V *= np.exp2(np.linspace(30, 0, 700))[None, :, None]
         case = Case(n=700, W=60, G=G, K=from_bits(ref.bits(K.astype(np.float32))), V=from_bits(ref.bits(V.astype(np.float32))))
         check(case, signed_queries(1, 1, 2 * G, [1, -1], 9))
+
+
+# ---- the end of the declared range ----------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("G", [1, 8, 16])
+@pytest.mark.parametrize("packed", [0, 1, None])
+@pytest.mark.parametrize("size", [59, -59])
+def test_sums_of_the_largest_and_smallest_values(G, packed, size):
+    """equal logits and values of one sign, between 2^58 and 2^60 (or 2^-60 and 2^-58), dozens of rows a warp: in bf16 only, in both forms, nearly
+    all in 4 bits"""
+    rng = np.random.default_rng(10)
+    V = rng.uniform(0.5, 1.99, (160, 700, 128)) * 2.0 ** size
+    K = np.zeros((160, 700, 128), np.float32)
+    K[:, 300:] = 0.45      # logits of 5.1 in the later rows: below what raises the reference, so their weights are above 1
+    case = Case(B=80, Hkv=2, n=700, W=30, G=G, packed=packed, K=from_bits(ref.bits(K)), V=from_bits(ref.bits(V.astype(np.float32))))
+    check(case, signed_queries(80, 1, 2 * G, [1], 11), sequences=(0, 77, 158, 159))
