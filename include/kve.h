@@ -341,7 +341,9 @@ int kvE_attach_q4(kvE_store* st, const kvE_q4_buffers* buf);
 /* Chunks [chunk_begin, chunk_end) of every sequence of `layer` to 4 bits, from their bf16 pages, which stay as they are
  * (kvE_reclaim_pages with KVE_RECLAIM_PACKED hands them back).  chunk_begin <= n_packed, chunk_end <= floor((n - W) / C): else
  * KVE_ERR_STATE.  KVE_ERR_GEOMETRY where S rows / 8 reaches 2^31 (take fewer chunks a call).  Neither summaries nor scores are needed.  Captured, a replay packs the same chunks again and
- * leaves the device's n_packed at chunk_end or more, or where it was if chunks before chunk_begin are not packed then. */
+ * leaves the device's n_packed at chunk_end or more, or where it was if chunks before chunk_begin are not packed then.
+ * A chunk whose bf16 page is gone (-1) keeps the copy that it has; without one its rows stand for NaN from then on.  Either sets KVE_ERR_CAPACITY in
+ * the status word, unless the keep list covers the chunk and leaves it out (KVE_RECLAIM_DISCARDED before packing: gated attention does not come to it). */
 int kvE_pack_chunks(kvE_store* st, int layer, int chunk_begin, int chunk_end, void* stream);
 
 /* What chunks [chunk_begin, chunk_end) stand for, rounded to bf16: k_out, v_out DEVICE bf16 [S][(chunk_end - chunk_begin) C][d], on 16

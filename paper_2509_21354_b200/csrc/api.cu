@@ -1069,7 +1069,8 @@ int kvE_pack_chunks(kvE_store* st, int layer, int chunk_begin, int chunk_end, vo
   if (chunk_end == chunk_begin) return KVE_OK;
   if (too_many_units(st, chunk_end - chunk_begin)) return KVE_ERR_GEOMETRY;
   Prof prof(st, KVE_K_PACK, static_cast<cudaStream_t>(stream));
-  const cudaError_t e = launch_pack(view(st, layer), q4_pages(st, layer), chunk_begin, chunk_end, static_cast<cudaStream_t>(stream));
+  const cudaError_t e = launch_pack(view(st, layer), q4_pages(st, layer), chunk_begin, chunk_end, reinterpret_cast<int32_t*>(static_cast<char*>(st->buf.workspace) + st->off_ticket),
+                                    static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return cuda_fail(st, e);
   if (chunk_end > ls.n_packed) ls.n_packed = chunk_end;
   return KVE_OK;

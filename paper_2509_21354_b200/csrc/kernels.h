@@ -93,8 +93,8 @@ struct Q4Pages {
   const int32_t* table;       // [S][max_chunks], this layer's
 };
 constexpr int Q4_UNIT_ROWS = 16, Q4_UNIT_BYTES = 1152, Q4_PAIR_BYTES = 2 * Q4_UNIT_BYTES;
-// chunks [t0, t1); the device's count of packed chunks goes up to t1
-cudaError_t launch_pack(const LayerView& v, const Q4Pages& p, int t0, int t1, cudaStream_t st);
+// chunks [t0, t1); the device's count of packed chunks goes up to t1.  ticket: one int, zero between launches
+cudaError_t launch_pack(const LayerView& v, const Q4Pages& p, int t0, int t1, int32_t* ticket, cudaStream_t st);
 cudaError_t launch_unpack(const LayerView& v, const Q4Pages& p, int t0, int t1, void* k_out, void* v_out, cudaStream_t st);
 // attention of T query tokens on G query heads a KV head.  Query rows go in `groups` of `cols`, one CTA each; every sequence is cut into parts_per_seq equal
 // parts, and `runs` CTAs per group share them; partials: (S + runs) groups records of `cols` rows of ATTN_PARTIAL_FLOATS; counters: S groups, zero between launches

@@ -78,32 +78,59 @@ __device__ __forceinline__ uint32_t q4_half(float c0, float c1, float c2, float 
   return __float_as_uint(fmaf(fmaf(c3, 16.f, c2), 256.f, fmaf(c1, 16.f, c0)) + 8388608.f);
 }
 
-__global__ void __launch_bounds__(PK_WARPS * 32) kve_pack_kernel(LayerView v, Q4Pages p, int t0, int n_chunks, int n_units, FastDiv by_units, FastDiv by_chunks) {
+// the keep list covers chunk t of sequence s and leaves it out: gated attention does not come to it
+__device__ __forceinline__ bool discarded(const LayerView& v, int s, int t) {
+  if (t >= *v.n_listed) return false;
+  const int32_t* kept = v.keep_idx + (long long)s * v.max_chunks;
+  int lo = 0, hi = v.keep_cnt[s];
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (kept[mid] < t) lo = mid + 1; else hi = mid;
+  }
+  return lo == v.keep_cnt[s] || kept[lo] != t;
+}
+
+__global__ void __launch_bounds__(PK_WARPS * 32) kve_pack_kernel(LayerView v, Q4Pages p, int t0, int n_chunks, int n_units, FastDiv by_units, FastDiv by_chunks,
+                                                                 int32_t* ticket) {
   __shared__ uint32_t codes[PK_WARPS][Q4_UNIT_ROWS * PK_PITCH];
+  __shared__ int had_packed;
   pdl_launch_dependents();
   pdl_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  if (blockIdx.x == 0 && threadIdx.x == 0) {      // (a replay may find another length, or fewer chunks packed: none is named that has no rows, no gap left)
-    const int had = *v.n_packed, now = min(t0 + n_chunks, v.seq_len[0] / v.C);
-    if (had >= t0 && now > had) *v.n_packed = now;
-  }
+  if (threadIdx.x == 0) had_packed = *reinterpret_cast<const volatile int32_t*>(v.n_packed);
   const int item = blockIdx.x * PK_WARPS + warp;
-  if (item >= n_units) return;
+  const bool live = item < n_units;
   const int per_chunk = v.C / Q4_UNIT_ROWS;
   const bool is_v = item & 1;
   const int x = (int)by_units.div((uint32_t)(item >> 1)), unit = (item >> 1) - x * per_chunk;
   const int s = (int)by_chunks.div((uint32_t)x), t = t0 + x - s * n_chunks;
-  const long long at = (long long)s * v.max_chunks + t, page = v.page_table[at], page4 = p.table[at];
-  if (page < 0 || page >= v.n_pages || page4 < 0 || page4 >= p.n_pages) {
-    if (lane == 0) set_status(v.status, ERR_CAPACITY);
-    return;
-  }
+  const long long at = (long long)s * v.max_chunks + t, page = live ? v.page_table[at] : -1, page4 = live ? p.table[at] : -1;
+  const bool source = page >= 0 && page < v.n_pages, target = page4 >= 0 && page4 < p.n_pages, whole = source && target;
   const int half = lane >> 4, l16 = lane & 15;
-  const uint4* src = reinterpret_cast<const uint4*>((is_v ? v.v_pages : v.k_pages) + (page * v.C + unit * Q4_UNIT_ROWS) * D) + lane;
   uint8_t* dst = p.kv + (page4 * per_chunk + unit) * Q4_PAIR_BYTES + (is_v ? Q4_UNIT_BYTES : 0);
   uint4 row[8];
+  if (whole) {
+    const uint4* src = reinterpret_cast<const uint4*>((is_v ? v.v_pages : v.k_pages) + (page * v.C + unit * Q4_UNIT_ROWS) * D) + lane;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) row[i] = __ldcs(src + i * 32);      // rows 2 i + half
+    for (int i = 0; i < 8; ++i) row[i] = __ldcs(src + i * 32);      // rows 2 i + half
+  }
+  // The count of packed chunks goes up when every CTA has read it: a chunk that was not packed before and whose rows are gone has no copy that could stay.
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const int arrived = atomicAdd(ticket, 1);      // (no fence: the barrier has waited for the read, which is all that the last one's write must not pass)
+    if (arrived == (int)gridDim.x - 1) {      // (a replay may find another length, or fewer chunks packed: none is named that has no rows, no gap left)
+      const int now = min(t0 + n_chunks, v.seq_len[0] / v.C);
+      if (had_packed >= t0 && now > had_packed) *v.n_packed = now;
+      *ticket = 0;      // clean for the next launch
+    }
+  }
+  if (!live) return;
+  if (!whole) {      // (warp by warp)
+    if (!source && target && t >= had_packed)      // 16 rows of two groups that stand for NaN, not for what the page held before
+      *reinterpret_cast<uint32_t*>(dst + Q4_CODE_BYTES + lane * 4) = 0x7fff7fffu;
+    if (lane == 0 && !(page == -1 && target && discarded(v, s, t))) set_status(v.status, ERR_CAPACITY);
+    return;
+  }
   // (largest, -smallest) of this lane's part of row 2 i + half; then of the whole group, lane by lane: lane 8 g + i has group g of the rows 2 i and 2 i + 1
   uint32_t m[8];
 #pragma unroll
@@ -218,11 +245,11 @@ static unsigned pack_grid(const LayerView& v, int chunks, int& n_units, FastDiv&
   return (unsigned)((n_units + PK_WARPS - 1) / PK_WARPS);
 }
 
-cudaError_t launch_pack(const LayerView& v, const Q4Pages& p, int t0, int t1, cudaStream_t st) {
+cudaError_t launch_pack(const LayerView& v, const Q4Pages& p, int t0, int t1, int32_t* ticket, cudaStream_t st) {
   int n_units;
   FastDiv by_units, by_chunks;
   const unsigned grid = pack_grid(v, t1 - t0, n_units, by_units, by_chunks);
-  return launch_pdl(kve_pack_kernel, dim3(grid), dim3(PK_WARPS * 32), 0, st, v, p, t0, t1 - t0, n_units, by_units, by_chunks);
+  return launch_pdl(kve_pack_kernel, dim3(grid), dim3(PK_WARPS * 32), 0, st, v, p, t0, t1 - t0, n_units, by_units, by_chunks, ticket);
 }
 
 cudaError_t launch_unpack(const LayerView& v, const Q4Pages& p, int t0, int t1, void* k_out, void* v_out, cudaStream_t st) {

@@ -1,0 +1,99 @@
+"""The cache in 4 bits beside pages that were handed back."""
+import numpy as np
+import pytest
+import torch
+
+from tests import reference_q4 as ref
+from tests.test_gpu_q4 import Case, as_bits, every_third, from_bits, normal, numbers
+from tests.test_gpu_q4_sizes import check, expected
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- chunks whose bf16 rows are gone ---------------------------------------------------------------------------------------------------
+
+def stale_copies(st):
+    """4-bit pages that look like good ones: an earlier owner's"""
+    st.kv4_pages.fill_(0x11)
+
+
+def test_discarded_chunks_handed_back_before_packing():
+    """nothing that gated attention reads is missing: no error; whoever reads the discarded chunks all the same gets NaN"""
+    case = Case(n=700, W=60, listed=9, keep=every_third, packed=0, Hkv=3, G=2, max_tokens=800)
+    st = case.st
+    stale_copies(st)
+    _, count = st.reclaim_pages(0, 0, 9, mode="discarded")
+    st.pack_chunks(0, 0, 9)
+    torch.cuda.synchronize()
+    gone = 9 * 3 - sum(len(k) for k in case.kept)
+    assert int(count) == gone and st.poll_status() == 0 and st.packed_chunks(0) == 9
+    case.packed = 9
+    q = normal((1, 1, 6, 128), 5)
+    check(case, q, dense=False)
+    for got, rows in zip(st.unpack_chunks(0, 0, 9), (case.K, case.V)):
+        got, want = numbers(got), ref.quantise(as_bits(rows)[:, :576])[0]
+        for s in range(3):
+            for t in range(9):
+                at = s, slice(64 * t, 64 * t + 64)
+                if t in case.kept[s]:
+                    assert (np.abs(got[at] - want[at]) <= (2.0 ** -8 + 2.0 ** -23) * np.abs(want[at]) + 2.0 ** -134).all()
+                else:
+                    assert np.isnan(got[at]).all()
+    assert torch.isnan(st.decode_attn_q4(0, q, dense=True)).all()      # every sequence misses a chunk
+    assert st.poll_status() == 0
+    st.append(0, normal((3, 64, 128), 20), normal((3, 64, 128), 21))      # and further on, with the chunks behind them
+    st.pack_chunks(0, 9, 10)
+    torch.cuda.synchronize()
+    assert st.poll_status() == 0 and st.packed_chunks(0) == 10
+
+
+@pytest.mark.parametrize("listed", [0, 9])
+def test_a_chunk_that_is_wanted_and_gone_is_flagged(listed):
+    case = Case(n=700, W=60, listed=listed, keep=lambda s, t: t != 1, packed=0, Hkv=2)
+    st = case.st
+    stale_copies(st)
+    st.page_table[0, 1, 4] = -1
+    st.pack_chunks(0, 0, 9)
+    torch.cuda.synchronize()
+    assert st.poll_status() == -3
+    case.packed = 9
+    q = normal((1, 1, 2, 128), 5)
+    for dense in (False, True):
+        got = numbers(st.decode_attn_q4(0, q, dense=dense))[0, 0]
+        assert np.isnan(got[1]).all()
+        want, _, bound, _ = expected(case, numbers(q), dense, sequences=(0,))
+        assert (np.abs(got[0] - want[0, 0, 0]) <= bound[0, 0, 0]).all()
+    k, v = st.unpack_chunks(0, 4, 5)
+    assert torch.isnan(k[1]).all() and torch.isnan(v[1]).all() and torch.isfinite(k[0]).all() and torch.isfinite(v[0]).all()
+
+
+def test_a_page_that_is_out_of_range_is_flagged_even_if_discarded():
+    case = Case(n=700, W=60, listed=9, keep=lambda s, t: t != 1, packed=0)
+    st = case.st
+    st.page_table[0, 0, 1] = 1 << 30
+    st.pack_chunks(0, 0, 9)
+    torch.cuda.synchronize()
+    assert st.poll_status() == -3
+
+
+def test_replayed_packing_keeps_the_copies_of_chunks_handed_back():
+    case = Case(n=700, W=60, packed=0)
+    st = case.st
+    stale_copies(st)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        st.pack_chunks(0, 0, 8)
+    graph.replay()
+    st.reclaim_pages(0, 2, 5, mode="packed")
+    torch.cuda.synchronize()
+    assert st.poll_status() == 0
+    case.packed = 8
+    q = normal((1, 1, 2, 128), 5)
+    check(case, q)
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert st.poll_status() == -3
+    check(case, q)
+    assert st.packed_chunks(0) == 8
