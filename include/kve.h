@@ -228,7 +228,9 @@ int kvE_compact_topk(kvE_store* st, int layer, int k, void* stream);
  *   mode KVE_RECLAIM_GATED:     pages of all chunks in the range; needs cfg.attend == KVE_ATTEND_SUMMARY,
  *                               where a retained chunk is read through its one summary row;
  *   mode KVE_RECLAIM_PACKED:    the bf16 pages of all chunks in the range, which need not be covered by the keep list but
- *                               must all be held in 4 bits (kvE_pack_chunks); kvE_decode_attn_q4 does not read them.
+ *                               must all be held in 4 bits (kvE_pack_chunks); kvE_decode_attn_q4 does not read them.  What the
+ *                               device does not hold in 4 bits (packing that was captured and has not run, a replayed kvE_set_len,
+ *                               no 4-bit page) keeps its page, and KVE_ERR_CAPACITY is set in the status word.
  * free_list: DEVICE int32 [capacity], receives the page ids, sequences in order, chunks ascending;
  * free_count: DEVICE int32, receives how many.  The page_table entries handed back become -1 (the
  * library writes the caller's page table here); entries that are already -1 are skipped.  If the

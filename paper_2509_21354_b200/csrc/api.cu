@@ -185,6 +185,10 @@ LayerView view(const kvE_store* st, int layer) {
   v.B = c.B; v.H = c.Hkv; v.S = st->S; v.C = c.C; v.max_chunks = st->max_chunks; v.max_tokens = c.max_tokens;
   return v;
 }
+Q4Pages q4_pages(const kvE_store* st, int layer) {
+  return Q4Pages{static_cast<uint8_t*>(st->q4.kv4_pages), st->q4.n_pages4,
+                 st->q4.page_table4 + (size_t)layer * st->S * st->max_chunks};
+}
 
 int stale_chunks(const kvE_config& c, int n) { return n > c.W ? (n - c.W) / c.C : 0; }
 
@@ -681,7 +685,7 @@ int kvE_reclaim_pages(kvE_store* st, int layer, int chunk_begin, int chunk_end, 
     return e == cudaSuccess ? KVE_OK : cuda_fail(st, e);
   }
   int32_t* scratch = reinterpret_cast<int32_t*>(static_cast<char*>(st->buf.workspace) + st->off_reclaim);
-  cudaError_t e = launch_reclaim(view(st, layer), chunk_begin, chunk_end, ls.tau, mode == KVE_RECLAIM_PACKED ? KVE_RECLAIM_GATED : mode, scratch, free_list, capacity, free_count,
+  cudaError_t e = launch_reclaim(view(st, layer), mode == KVE_RECLAIM_PACKED ? q4_pages(st, layer) : Q4Pages{}, chunk_begin, chunk_end, ls.tau, mode, scratch, free_list, capacity, free_count,
                                  static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? KVE_OK : cuda_fail(st, e);
 }
@@ -989,10 +993,6 @@ int check_q4(const kvE_config* c, int max_query_tokens) {
   if (max_query_tokens < 1) return KVE_ERR_ARG;
   if (c->C % Q4_UNIT_ROWS != 0 || (long long)max_query_tokens * (c->Hq / c->Hkv) > Q4_MAX_ROWS) return KVE_ERR_GEOMETRY;
   return KVE_OK;
-}
-Q4Pages q4_pages(const kvE_store* st, int layer) {
-  return Q4Pages{static_cast<uint8_t*>(st->q4.kv4_pages), st->q4.n_pages4,
-                 st->q4.page_table4 + (size_t)layer * st->S * st->max_chunks};
 }
 
 // units of keys and of values in a call: the kernels count them in 32 bits

@@ -193,14 +193,17 @@ cudaError_t launch_compact_topk(const LayerView& v, int n_chunks, int k, void* k
 
 // ---- kvE_reclaim_pages kernels (Sec. 3.3, memory ratio n / (W + M)): pages of gated chunks go back to the caller ----
 // A chunk gives its page back if it was discarded (score < tau) or, with mode 1, in any case (retained
-// chunks live on as their summary row).  Free-list order: sequences in order, chunks ascending, so the
+// chunks live on as their summary row), or, with mode 2, if it has a copy in 4 bits.  Free-list order: sequences in order, chunks ascending, so the
 // result is unique.  count -> scan -> scatter; the scatter does nothing if the list would overflow.
-__device__ __forceinline__ bool reclaimable(const LayerView& v, int s, int t, float tau, int mode) {
+// (The host's count of packed chunks is not enough for mode 2: packing may have been captured only, a replay may have lowered the device's count.)
+__device__ __forceinline__ bool reclaimable(const LayerView& v, const Q4Pages& p, int s, int t, float tau, int mode) {
   const long long i = (long long)s * v.max_chunks + t;
-  return (mode == 1 || !(v.scores[i] >= tau)) && v.page_table[i] >= 0;
+  if (v.page_table[i] < 0) return false;
+  if (mode != 2) return mode == 1 || !(v.scores[i] >= tau);
+  return t < *v.n_packed && p.table[i] >= 0 && p.table[i] < p.n_pages;
 }
 
-__global__ void __launch_bounds__(COMPACT_WARPS * 32) kve_reclaim_count_kernel(LayerView v, int t0, int t1, float tau, int mode,
+__global__ void __launch_bounds__(COMPACT_WARPS * 32) kve_reclaim_count_kernel(LayerView v, Q4Pages p, int t0, int t1, float tau, int mode,
                                                                               int32_t* counts) {
   pdl_launch_dependents();
   pdl_wait();
@@ -210,7 +213,9 @@ __global__ void __launch_bounds__(COMPACT_WARPS * 32) kve_reclaim_count_kernel(L
   int n = 0;
   for (int tb = t0; tb < t1; tb += 32) {
     const int t = tb + lane;
-    n += __popc(__ballot_sync(0xffffffffu, t < t1 && reclaimable(v, s, t, tau, mode)));
+    const bool give = t < t1 && reclaimable(v, p, s, t, tau, mode);
+    n += __popc(__ballot_sync(0xffffffffu, give));
+    if (mode == 2 && t < t1 && !give && v.page_table[(long long)s * v.max_chunks + t] >= 0) set_status(v.status, ERR_CAPACITY);      // the only copy of its rows: it stays
   }
   if (lane == 0) counts[s] = n;
 }
@@ -257,7 +262,7 @@ __global__ void __launch_bounds__(1024) kve_reclaim_scan_kernel(const int32_t* c
   }
 }
 
-__global__ void __launch_bounds__(COMPACT_WARPS * 32) kve_reclaim_scatter_kernel(LayerView v, int t0, int t1, float tau, int mode,
+__global__ void __launch_bounds__(COMPACT_WARPS * 32) kve_reclaim_scatter_kernel(LayerView v, Q4Pages p, int t0, int t1, float tau, int mode,
                                                                                 const int32_t* offsets, int32_t* free_list) {
   pdl_launch_dependents();
   pdl_wait();
@@ -268,7 +273,7 @@ __global__ void __launch_bounds__(COMPACT_WARPS * 32) kve_reclaim_scatter_kernel
   int base = offsets[s];
   for (int tb = t0; tb < t1; tb += 32) {
     const int t = tb + lane;
-    const bool give = t < t1 && reclaimable(v, s, t, tau, mode);
+    const bool give = t < t1 && reclaimable(v, p, s, t, tau, mode);
     const unsigned mask = __ballot_sync(0xffffffffu, give);
     if (give) {
       free_list[base + __popc(mask & ((1u << lane) - 1u))] = table[t];
@@ -278,17 +283,17 @@ __global__ void __launch_bounds__(COMPACT_WARPS * 32) kve_reclaim_scatter_kernel
   }
 }
 
-cudaError_t launch_reclaim(const LayerView& v, int t0, int t1, float tau, int mode, int32_t* scratch, int32_t* free_list,
+cudaError_t launch_reclaim(const LayerView& v, const Q4Pages& p, int t0, int t1, float tau, int mode, int32_t* scratch, int32_t* free_list,
                            long long capacity, int32_t* free_count, cudaStream_t st) {
   int32_t* counts = scratch;
   int32_t* offsets = scratch + v.S;
   const dim3 grid((v.S + COMPACT_WARPS - 1) / COMPACT_WARPS), block(COMPACT_WARPS * 32);
-  cudaError_t e = launch_pdl(kve_reclaim_count_kernel, grid, block, 0, st, v, t0, t1, tau, mode, counts);
+  cudaError_t e = launch_pdl(kve_reclaim_count_kernel, grid, block, 0, st, v, p, t0, t1, tau, mode, counts);
   if (e == cudaSuccess)
     e = launch_pdl(kve_reclaim_scan_kernel, dim3(1), dim3(1024), 0, st, (const int32_t*)counts, v.S, offsets, capacity, free_count,
                    v.status);
   if (e == cudaSuccess)
-    e = launch_pdl(kve_reclaim_scatter_kernel, grid, block, 0, st, v, t0, t1, tau, mode, (const int32_t*)offsets, free_list);
+    e = launch_pdl(kve_reclaim_scatter_kernel, grid, block, 0, st, v, p, t0, t1, tau, mode, (const int32_t*)offsets, free_list);
   return e;
 }
 

@@ -133,7 +133,8 @@ cudaError_t launch_gate_step(const LayerView& v, int t, const uint16_t* W_ih, co
 // what attention reads until the next keep list
 cudaError_t launch_compact(const LayerView& v, int n_chunks, float tau, void* kkept, void* vkept, cudaStream_t st);
 cudaError_t launch_compact_topk(const LayerView& v, int n_chunks, int k, void* kkept, void* vkept, cudaStream_t st);
-cudaError_t launch_reclaim(const LayerView& v, int t0, int t1, float tau, int mode, int32_t* scratch, int32_t* free_list,
+// mode: KVE_RECLAIM_*; p is read for KVE_RECLAIM_PACKED only
+cudaError_t launch_reclaim(const LayerView& v, const Q4Pages& p, int t0, int t1, float tau, int mode, int32_t* scratch, int32_t* free_list,
                            long long capacity, int32_t* free_count, cudaStream_t st);
 // parts_per_seq: equal parts every sequence is cut into; grid: CTAs that share the S * parts_per_seq parts;
 // partials: S + grid records of ATTN_PARTIAL_FLOATS

@@ -1,4 +1,4 @@
-"""The cache in 4 bits beside pages that were handed back."""
+"""The cache in 4 bits beside pages that were handed back and counts that only the device knows."""
 import numpy as np
 import pytest
 import torch
@@ -97,3 +97,48 @@ def test_replayed_packing_keeps_the_copies_of_chunks_handed_back():
     assert st.poll_status() == -3
     check(case, q)
     assert st.packed_chunks(0) == 8
+
+
+# ---- counts that the host has not heard of ---------------------------------------------------------------------------------------------
+
+def test_bf16_pages_stay_where_the_device_holds_no_copy():
+    """packing that was captured and never ran, and a replayed kvE_set_len: the only copy of a chunk is not handed back"""
+    case = Case(n=700, W=60, packed=0)
+    st, table = case.st, case.st.page_table.clone()
+    q = normal((1, 1, 2, 128), 5)
+    torch.cuda.synchronize()
+    pack, cut = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(pack):
+        st.pack_chunks(0, 0, 9)
+    _, count = st.reclaim_pages(0, 0, 9, mode="packed")
+    torch.cuda.synchronize()
+    assert int(count) == 0 and torch.equal(st.page_table, table) and st.poll_status() == -3
+    check(case, q)
+    pack.replay()
+    case.packed = 9
+    check(case, q)
+    with torch.cuda.graph(cut):
+        st.set_len(0, 300)
+    st.set_len(0, 700)
+    st.adopt_device_state(0)
+    st.pack_chunks(0, 0, 9)
+    cut.replay()                                            # the device: chunks 0 to 3, the host: nine
+    free, count = st.reclaim_pages(0, 0, 9, mode="packed")
+    torch.cuda.synchronize()
+    assert int(count) == 8 and (st.page_table[0, :, :4] == -1).all() and torch.equal(st.page_table[0, :, 4:], table[0, :, 4:])
+    assert sorted(free[:8].tolist()) == sorted(table[0, :, :4].flatten().tolist())
+    assert st.poll_status() == -3
+
+
+def test_bf16_pages_stay_where_there_is_no_4_bit_page():
+    case = Case(n=700, W=60, packed=0)
+    st, table = case.st, case.st.page_table.clone()
+    for bad in (-1, 1 << 30):
+        st.page_table4[0, 1, 2] = bad
+        st.pack_chunks(0, 0, 9)
+        torch.cuda.synchronize()
+        assert st.poll_status() == -3
+        _, count = st.reclaim_pages(0, 2, 3, mode="packed")
+        torch.cuda.synchronize()
+        assert int(count) == (1 if bad == -1 else 0) and st.poll_status() == -3
+        assert st.page_table[0, 0, 2] == -1 and st.page_table[0, 1, 2] == table[0, 1, 2]
