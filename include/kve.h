@@ -349,7 +349,8 @@ int kvE_attach_q4(kvE_store* st, const kvE_q4_buffers* buf);
 int kvE_pack_chunks(kvE_store* st, int layer, int chunk_begin, int chunk_end, void* stream);
 
 /* What chunks [chunk_begin, chunk_end) stand for, rounded to bf16: k_out, v_out DEVICE bf16 [S][(chunk_end - chunk_begin) C][d], on 16
- * bytes: what kvE_append takes.  The way back, to roll into a packed chunk or to move the history elsewhere. */
+ * bytes: what kvE_append takes.  The way back, to roll into a packed chunk or to move the history elsewhere.  Rows of chunks that the device does
+ * not hold in 4 bits (KVE_RECLAIM_PACKED) are not written, and KVE_ERR_CAPACITY is set in the status word. */
 int kvE_unpack_chunks(kvE_store* st, int layer, int chunk_begin, int chunk_end, void* k_out, void* v_out, void* stream);
 
 /* Host-side view: chunks of `layer` held in 4 bits. */

@@ -193,9 +193,9 @@ __global__ void __launch_bounds__(PK_WARPS * 32) kve_unpack_kernel(LayerView v, 
   const int per_chunk = v.C / Q4_UNIT_ROWS;
   const bool is_v = item & 1;
   const int x = (int)by_units.div((uint32_t)(item >> 1)), unit = (item >> 1) - x * per_chunk;
-  const int s = (int)by_chunks.div((uint32_t)x);
-  const long long page4 = p.table[(long long)s * v.max_chunks + t0 + x - s * n_chunks];
-  if (page4 < 0 || page4 >= p.n_pages) {
+  const int s = (int)by_chunks.div((uint32_t)x), t = t0 + x - s * n_chunks;
+  const long long page4 = p.table[(long long)s * v.max_chunks + t];
+  if (page4 < 0 || page4 >= p.n_pages || t >= *v.n_packed) {      // (packing that was captured and has not run is in the host's count already)
     if (lane == 0) set_status(v.status, ERR_CAPACITY);
     return;
   }

@@ -142,3 +142,23 @@ def test_bf16_pages_stay_where_there_is_no_4_bit_page():
         torch.cuda.synchronize()
         assert int(count) == (1 if bad == -1 else 0) and st.poll_status() == -3
         assert st.page_table[0, 0, 2] == -1 and st.page_table[0, 1, 2] == table[0, 1, 2]
+
+
+def test_unpacking_what_the_device_does_not_hold_is_flagged():
+    case = Case(n=700, W=60, packed=0)
+    st = case.st
+    stale_copies(st)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        st.pack_chunks(0, 0, 9)
+    out = [torch.full((2, 9 * 64, 128), 9.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    st.unpack_chunks(0, 0, 9, *out)
+    torch.cuda.synchronize()
+    assert st.poll_status() == -3 and all((x == 9.0).all() for x in out)
+    graph.replay()
+    st.unpack_chunks(0, 0, 9, *out)
+    torch.cuda.synchronize()
+    assert st.poll_status() == 0
+    want = ref.quantise(as_bits(case.V)[:, :576])[0]
+    assert (np.abs(numbers(out[1]) - want) <= (2.0 ** -8 + 2.0 ** -23) * np.abs(want) + 2.0 ** -134).all()
