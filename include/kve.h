@@ -362,7 +362,8 @@ int kvE_packed_chunks(const kvE_store* st, int layer, int* n_packed);
  * included).  The position of the list, of the packed chunks and of the newest row are taken from the device: a captured launch
  * stays valid across triggers and further packing.  cfg.attend does not matter.
  *   causal != 0: the block's tokens are the newest of the cache and see it up to themselves; KVE_ERR_STATE if fewer rows than
- *   n_query_tokens lie behind the packed and listed chunks (a replay that comes to that sets KVE_ERR_CAPACITY).
+ *   n_query_tokens lie behind the packed and listed chunks (a replay that comes to that sets KVE_ERR_CAPACITY).  Keys and values of a token are nothing to the
+ *   tokens in front of it, infinities and NaN included.
  *   Sums in fp32, weights of packed rows to 11 bits (of bf16 rows to 16), one bf16 rounding of the result: values between 2^-60 and 2^60 in
  *   magnitude, or 0.  (Scales below that lose bits; sums of larger bf16 rows beside them may overflow.)  A row that sees nothing gives 0 and lse = -inf.
  *   q, out: DEVICE bf16 [B][n_query_tokens][Hq][d], on 16 bytes; lse: DEVICE fp32 [B][n_query_tokens][Hq] or NULL.

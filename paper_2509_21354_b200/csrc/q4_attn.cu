@@ -114,6 +114,8 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
   return d;
 }
 
+// which halves of a bf16 pair are an infinity or a NaN, as a mask of bits
+__device__ __forceinline__ uint32_t not_finite(uint32_t w) { return ((w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u); }
 // word i of four (i known at compile time)
 __device__ __forceinline__ uint32_t word_of(const uint4& w, int i) { return i == 0 ? w.x : (i == 1 ? w.y : (i == 2 ? w.z : w.w)); }
 // folds a state (accumulator, reference, sum) into one with reference `top`
@@ -437,6 +439,32 @@ __global__ void __launch_bounds__(QaShape<COLS>::WARPS * 32, 1) kve_decode_attn_
         if (++stage == STAGES) { stage = 0; phase ^= 1u; }
       }
     };
+    // A causal block's newest rows, which not all query rows see: a product with a weight of 0 would still make NaN of a value that is not finite.  Whether the tile of
+    // `rows` bf16 rows from position pos has any of those ...
+    auto hides = [&](int rows, int pos, const unsigned char* base) {
+      if (!a.causal || pos + rows - 1 <= progress[CW + 1] - a.T) return false;
+      uint32_t any = 0u;
+      if (g8 < rows)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint4 w = *reinterpret_cast<const uint4*>(base + QA_V_OFF + g8 * ROW_BYTES + i * 64 + t4 * 16);
+          any |= not_finite(w.x) | not_finite(w.y) | not_finite(w.z) | not_finite(w.w);
+        }
+      return (bool)__any_sync(0xffffffffu, any != 0u);
+    };
+    // ... and when every lane has added those that its query rows see, zeros in their place
+    auto clear = [&](int rows, const unsigned char* base) {
+      __syncwarp();
+      if (g8 < rows)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          uint4* p = reinterpret_cast<uint4*>(const_cast<unsigned char*>(base) + QA_V_OFF + g8 * ROW_BYTES + i * 64 + t4 * 16);
+          const uint4 w = *p;
+          *p = make_uint4(w.x & ~not_finite(w.x), w.y & ~not_finite(w.y), w.z & ~not_finite(w.z), w.w & ~not_finite(w.w));
+        }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // (the stage is filled by a bulk copy again)
+      __syncwarp();
+    };
     if constexpr (!MANY) {
       // ---- up to eight query rows: the cache on the M side, the queries in the columns.  Up to four (DUO): rows 0 to 3 twice, where the products with packed keys and
       // values have group 0 in the columns below 4 and group 1 in those from 4 on ----
@@ -690,6 +718,27 @@ __global__ void __launch_bounds__(QaShape<COLS>::WARPS * 32, 1) kve_decode_attn_
 
       // a tile of `rows` <= 8 bf16 rows, the first at position pos
       auto bf16_rows = [&](int rows, int pos, const unsigned char* base) {
+        if (hides(rows, pos, base)) {
+#pragma unroll 1
+          for (int j = 0; j < rows; ++j)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const uint4 w = *reinterpret_cast<const uint4*>(base + QA_V_OFF + j * ROW_BYTES + h * 128 + g8 * 16);
+#pragma unroll
+              for (int m = 0; m < 4; ++m) {
+                const uint32_t v2 = word_of(w, m), bad = not_finite(v2);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                  for (int c = 0; c < 2; ++c) {
+                    if (pos + j > last_pos(nt, c)) continue;
+                    if (bad & 0xffffu) acc[nt][4 * h + m][c] += bf16lo(v2);
+                    if (bad >> 16) acc[nt][4 * h + m][2 + c] += bf16hi(v2);
+                  }
+              }
+            }
+          clear(rows, base);
+        }
         float x[NT][2];
         {
           float d[NT][2][4];
@@ -1012,6 +1061,27 @@ __global__ void __launch_bounds__(QaShape<COLS>::WARPS * 32, 1) kve_decode_attn_
 
       // `rows` <= 8 bf16 rows, the first at position pos
       auto bf16_rows = [&](int rows, int pos, const unsigned char* base) {
+        if (hides(rows, pos, base)) {
+#pragma unroll 1
+          for (int j = 0; j < rows; ++j)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+              for (int c = 0; c < 2; ++c) {
+                const uint4 w = *reinterpret_cast<const uint4*>(base + QA_V_OFF + j * ROW_BYTES + h * 128 + (2 * t4 + c) * 16);
+#pragma unroll
+                for (int m = 0; m < 4; ++m) {
+                  const uint32_t v2 = word_of(w, m), bad = not_finite(v2);
+#pragma unroll
+                  for (int r = 0; r < 2; ++r) {
+                    if (pos + j > last_pos(r)) continue;
+                    if (bad & 0xffffu) acc[8 * h + 2 * m][2 * r + c] += bf16lo(v2);
+                    if (bad >> 16) acc[8 * h + 2 * m + 1][2 * r + c] += bf16hi(v2);
+                  }
+                }
+              }
+          clear(rows, base);
+        }
         float d[2][4], x[1][4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {

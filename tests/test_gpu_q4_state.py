@@ -1,4 +1,4 @@
-"""The cache in 4 bits beside pages that were handed back and counts that only the device knows."""
+"""The cache in 4 bits beside pages that were handed back, counts that only the device knows and rows that are not seen."""
 import numpy as np
 import pytest
 import torch
@@ -162,3 +162,29 @@ def test_unpacking_what_the_device_does_not_hold_is_flagged():
     assert st.poll_status() == 0
     want = ref.quantise(as_bits(case.V)[:, :576])[0]
     assert (np.abs(numbers(out[1]) - want) <= (2.0 ** -8 + 2.0 ** -23) * np.abs(want) + 2.0 ** -134).all()
+
+
+# ---- rows that are not seen ------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("T,G", [(4, 1), (7, 1), (2, 2), (16, 1), (7, 4), (5, 8)])
+@pytest.mark.parametrize("n", [40, 333, 700])
+def test_causal_blocks_with_rows_that_are_not_finite(T, G, n):
+    """keys and values of a token are nothing to the tokens in front of it"""
+    K, V = as_bits(normal((2, n, 128), 2)).copy(), as_bits(normal((2, n, 128), 3)).copy()
+    V[0, n - 1, 5], V[0, n - 1, 70] = 0x7F80, 0x7FC0
+    K[1, n - 1] = 0x7FC0
+    V[1, n - T // 2, :] = 0xFF80
+    case = Case(n=n, W=60, T=T, G=G, K=from_bits(K), V=from_bits(V))
+    q = normal((1, T, 2 * G, 128), 4)
+    got = numbers(case.st.decode_attn_q4(0, q, dense=True, causal=True))
+    assert case.st.poll_status() == 0
+    want, _, bound, _ = expected(case, numbers(q), True, True)
+    for s, first in ((0, T - 1), (1, T - T // 2)):          # the first token that sees one of them
+        heads = slice(s * G, s * G + G)
+        seen = got[0, :first, heads]
+        assert seen.size and (np.abs(seen - want[0, :first, heads]) <= bound[0, :first, heads]).all()
+    assert np.isposinf(got[0, T - 1, :G, 5]).all() and np.isnan(got[0, T - 1, :G, 70]).all()
+    assert np.isfinite(np.delete(got[0, T - 1, :G], [5, 70], axis=-1)).all()
+    assert np.isnan(got[0, T - 1, G:]).all()
+    if T // 2 > 1:
+        assert np.isneginf(got[0, T - T // 2:T - 1, G:]).all()
