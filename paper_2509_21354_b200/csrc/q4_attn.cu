@@ -1019,26 +1019,32 @@ __global__ void __launch_bounds__(QaShape<COLS>::WARPS * 32, 1) kve_decode_attn_
 #pragma unroll
           for (int i = 2; i < 4; ++i) x[i][0] = x[i][1] = x[i][2] = x[i][3] = -INFINITY;
         }
-        uint4 vh[4];               // scale and lowest number of both groups of the keys 2 t4 and 2 t4 + 1, values
+        // scale and lowest number of both groups of the keys 2 t4 and 2 t4 + 1 of the i-th eight, values (from shared memory every time)
+        auto head = [&](int i) {
+          return i >= 2 && !whole ? make_uint4(0u, 0u, 0u, 0u)
+                                  : *reinterpret_cast<const uint4*>(base + (i >> 1) * Q4_PAIR_BYTES + Q4_UNIT_BYTES + Q4_CODE_BYTES + (i & 1) * 64 + 16 * t4);
+        };
         uint32_t most0 = 0u, most1 = 0u;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          vh[i] = *reinterpret_cast<const uint4*>(base + (i >> 1) * Q4_PAIR_BYTES + Q4_UNIT_BYTES + Q4_CODE_BYTES + (i & 1) * 64 + 16 * t4);
-          if (i >= 2 && !whole) vh[i] = make_uint4(0u, 0u, 0u, 0u);
-          most0 = max_bf16x2(most0, max_bf16x2(vh[i].x, vh[i].z));
-          most1 = max_bf16x2(most1, max_bf16x2(vh[i].y, vh[i].w));
+          const uint4 w = head(i);
+          most0 = max_bf16x2(most0, max_bf16x2(w.x, w.z));
+          most1 = max_bf16x2(most1, max_bf16x2(w.y, w.w));
         }
-        weigh(x, bf16lo(most0), bf16lo(most1), [&](int i, int k, int h) { return bf16lo(k ? (h ? vh[i].w : vh[i].z) : (h ? vh[i].y : vh[i].x)); });
+        weigh(x, bf16lo(most0), bf16lo(most1), [&](int i, int k, int h) { const uint4 w = head(i); return bf16lo(k ? (h ? w.w : w.z) : (h ? w.y : w.x)); });
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
+          const float2 F2 = make_float2(bf16lo(F[h]), bf16hi(F[h]));
           uint32_t A[2][4];        // weights times scale
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const uint32_t wa = h ? vh[i].y : vh[i].x, wb = h ? vh[i].w : vh[i].z;
+            const uint4 vh = head(i);
+            const uint32_t wa = h ? vh.y : vh.x, wb = h ? vh.w : vh.z;
             const float sa = bf16lo(wa), sb = bf16lo(wb), lo_a = bf16hi(wa), lo_b = bf16hi(wb);
+            const float2 fa = mul2(make_float2(sa, sa), F2), fb = mul2(make_float2(sb, sb), F2);
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
-              A[i >> 1][2 * (i & 1) + r] = pack_f16x2(x[i][2 * r] * (sa * (r ? bf16hi(F[h]) : bf16lo(F[h]))), x[i][2 * r + 1] * (sb * (r ? bf16hi(F[h]) : bf16lo(F[h]))));
+              A[i >> 1][2 * (i & 1) + r] = pack_f16x2(x[i][2 * r] * (r ? fa.y : fa.x), x[i][2 * r + 1] * (r ? fb.y : fb.x));
               zs[r][h] = fmaf(x[i][2 * r], lo_a, fmaf(x[i][2 * r + 1], lo_b, zs[r][h]));
             }
           }
