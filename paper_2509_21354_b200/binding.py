@@ -176,6 +176,19 @@ def _stream(st, stream=None) -> int:
     return torch._C._cuda_getCurrentRawStream(st.device_index) if stream is None else stream.cuda_stream
 
 
+def _result(st, shape, stream, dtype=_BF16, fill=torch.empty):
+    """A tensor for a result.  Of a call on a stream of its own it is that stream's: a block that the current stream has given back may
+    still be in use there.  (And the current stream will read it: it is not given out again before that has run.)"""
+    device = torch.device("cuda", st.device_index)
+    current = None if stream is None else torch.cuda.current_stream(device)
+    if stream is None or stream.cuda_stream == current.cuda_stream:
+        return fill(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = fill(shape, dtype=dtype, device=device)
+    t.record_stream(current)
+    return t
+
+
 def _p(t) -> int:
     if t is None:
         return 0
@@ -388,7 +401,7 @@ class Store:
     def decode_step(self, layer, k_new, v_new, q, out=None, lse=None, scale=None, n_reserve=0, stream=None):
         """append one token per sequence (k_new, v_new: bf16 [S, 128]) at the device-held length and attend, one launch"""
         if out is None:
-            out = torch.empty_like(q)
+            out = torch.empty_like(q) if stream is None else _result(self, q.shape, stream)
         if self._decode_step is None:
             rc = self.lib.kvE_decode_step(self.handle, layer, _rows(k_new, self.row_shape), _rows(v_new, self.row_shape), _rows(q, self.row_shape),
                                           _p(out), _p(lse), _DEFAULT_SCALE if scale is None else scale, int(n_reserve), _stream(self, stream))
@@ -545,7 +558,7 @@ def kvE_compact_topk(st: Store, layer, k, stream=None):
 def _attn(fn_name, st, layer, q, out, lse, scale, stream):
     q_ptr = _rows(q, st.row_shape)
     if out is None:
-        out = torch.empty_like(q)
+        out = _result(st, q.shape, stream)
     rc = getattr(st.lib, fn_name)(st.handle, layer, q_ptr, _p(out), _p(lse), _DEFAULT_SCALE if scale is None else scale, _stream(st, stream))
     if rc:
         _check(fn_name, rc, st.handle)
@@ -565,7 +578,7 @@ def kvE_decode_attn_block(st: Store, layer, q, dense=False, out=None, lse=None, 
     lse, if given, is an fp32 [B, T, Hq] device tensor."""
     assert q.dtype == torch.bfloat16 and q.dim() == 4 and q.shape[0] == st.B and q.shape[2] == st.Hq and q.shape[3] == 128
     if out is None:
-        out = torch.empty_like(q)
+        out = _result(st, q.shape, stream)
     assert out.shape == q.shape and out.dtype == torch.bfloat16
     if lse is not None:
         assert lse.dtype == torch.float32 and tuple(lse.shape) == tuple(q.shape[:3])
@@ -582,7 +595,7 @@ def _strided_rows(st, t, heads) -> kvE_rows:
     return kvE_rows(t.data_ptr(), *(stride if size > 1 else 0 for stride, size in zip(t.stride()[:3], t.shape)))
 
 
-def _rope_arguments(st, q, k_new, v_new, rope, positions, q_out):
+def _rope_arguments(st, q, k_new, v_new, rope, positions, q_out, stream):
     n = k_new.shape[1]
     k, v = _strided_rows(st, k_new, st.H), _strided_rows(st, v_new, st.H)
     assert v_new.shape[1] == n and (q is not None or q_out is None)
@@ -591,7 +604,7 @@ def _rope_arguments(st, q, k_new, v_new, rope, positions, q_out):
         rows = _strided_rows(st, q, st.Hq)
         assert q.shape[1] == n
         if q_out is None:
-            q_out = torch.empty((st.B, n, st.Hq, 128), dtype=_BF16, device=q.device)
+            q_out = _result(st, (st.B, n, st.Hq, 128), stream)
         assert q_out.dtype is _BF16 and q_out.shape == (st.B, n, st.Hq, 128)
     if positions is not None:
         assert positions.dtype == torch.int32 and positions.shape == (st.B, n, rope.n_axes)
@@ -607,7 +620,7 @@ def kvE_append_rope(st: Store, layer, q, k_new, v_new, rope, positions=None, q_o
         if rc:
             _check("kvE_append_rope", rc, st.handle)
         return q_out, ready
-    rows, k, v, pos, n, q_out = _rope_arguments(st, q, k_new, v_new, rope, positions, q_out)
+    rows, k, v, pos, n, q_out = _rope_arguments(st, q, k_new, v_new, rope, positions, q_out, stream)
     ready = C.c_int(0)
     _check("kvE_append_rope", st.lib.kvE_append_rope(st.handle, layer, rows, k, v, pos, n, C.byref(rope.c), _p(q_out), C.byref(ready), _stream(st, stream)),
            st.handle)
@@ -620,7 +633,7 @@ def kvE_append_rope_next(st: Store, layer, q, k_new, v_new, rope, positions=None
         if rc:
             _check("kvE_append_rope_next", rc, st.handle)
         return q_out
-    rows, k, v, pos, n, q_out = _rope_arguments(st, q, k_new, v_new, rope, positions, q_out)
+    rows, k, v, pos, n, q_out = _rope_arguments(st, q, k_new, v_new, rope, positions, q_out, stream)
     _check("kvE_append_rope_next", st.lib.kvE_append_rope_next(st.handle, layer, rows, k, v, pos, n, int(n_reserve), C.byref(rope.c), _p(q_out),
                                                                _stream(st, stream)), st.handle)
     return q_out
@@ -634,7 +647,7 @@ def kvE_unpack_chunks(st: Store, layer, chunk_begin, chunk_end, k_out=None, v_ou
             _check("kvE_unpack_chunks", rc, st.handle)
         return k_out, v_out
     shape = (st.S, max(0, int(chunk_end) - int(chunk_begin)) * st.C, 128)
-    k_out, v_out = (torch.empty(shape, dtype=_BF16, device=st.device) if t is None else t for t in (k_out, v_out))
+    k_out, v_out = (_result(st, shape, stream) if t is None else t for t in (k_out, v_out))
     if shape[1] > 0:      # (an empty tensor has no address)
         _check("kvE_unpack_chunks", st.lib.kvE_unpack_chunks(st.handle, layer, int(chunk_begin), int(chunk_end), _rows(k_out, shape), _rows(v_out, shape),
                                                              _stream(st, stream)), st.handle)
@@ -650,7 +663,7 @@ def kvE_decode_attn_q4(st: Store, layer, q, dense=False, causal=False, out=None,
         return out
     assert q.dtype is _BF16 and q.dim() == 4 and q.shape[0] == st.B and q.shape[2:] == (st.Hq, 128)
     if out is None:
-        out = torch.empty_like(q)
+        out = _result(st, q.shape, stream)
     assert out.shape == q.shape and out.dtype is _BF16
     if lse is not None:
         assert lse.dtype == torch.float32 and lse.shape == q.shape[:3]
@@ -669,9 +682,9 @@ def kvE_reclaim_pages(st: Store, layer, chunk_begin, chunk_end, mode="discarded"
     capacity; allocated here for the whole range if omitted), free_count: int32 device tensor [1].
     Returns (free_list, free_count); the first free_count entries are valid once the stream has run."""
     if free_list is None:
-        free_list = torch.empty((max(1, st.S * max(chunk_end - chunk_begin, 0)),), dtype=torch.int32, device=st.device)
+        free_list = _result(st, (max(1, st.S * max(chunk_end - chunk_begin, 0)),), stream, torch.int32)
     if free_count is None:
-        free_count = torch.zeros((1,), dtype=torch.int32, device=st.device)
+        free_count = _result(st, (1,), stream, torch.int32, torch.zeros)
     assert free_list.dtype == torch.int32 and free_count.dtype == torch.int32
     _check("kvE_reclaim_pages", st.lib.kvE_reclaim_pages(st.handle, layer, int(chunk_begin), int(chunk_end), RECLAIM[mode],
                                                         _p(free_list), free_list.numel(), _p(free_count),

@@ -3,6 +3,8 @@
 // conversion of ten arguments by ctypes took 2.9 us of the 6.3 us that a call took, 1.0 here; 7 tokens call by call 95 -> 82 us.)
 #include <Python.h>
 #include <ATen/ops/empty.h>
+#include <c10/cuda/CUDACachingAllocator.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -109,14 +111,27 @@ bool shaped(PyObject* o, at::ScalarType type, at::IntArrayRef shape, long device
 }
 
 // (handle, device and stream of the calls below)
-struct Call { void* handle; long device; void* stream; };
+struct Call { void* handle; long device; void* stream; bool own_stream; };
 bool call_of(PyObject* handle, PyObject* device, PyObject* stream, Call* c) {
   c->handle = handle == Py_None ? nullptr : PyLong_AsVoidPtr(handle);
   c->device = PyLong_AsLong(device);
   c->stream = stream == Py_None ? nullptr : PyLong_AsVoidPtr(stream);
+  c->own_stream = stream != Py_None;
   if (PyErr_Occurred()) return false;
   if (stream == Py_None) c->stream = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)c->device).stream();
   return true;
+}
+// A bf16 tensor for a result.  Of a call on a stream of its own it is that stream's: a block that the current stream has given back may still be in use there.
+// (And the current stream will read it: it is not given out again before that has run.)
+at::Tensor result_of(const Call& c, at::IntArrayRef shape) {
+  const auto options = at::TensorOptions().dtype(at::kBFloat16).device(at::kCUDA, (c10::DeviceIndex)c.device);
+  if (!c.own_stream) return at::empty(shape, options);
+  const auto current = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)c.device);
+  if (current.stream() == c.stream) return at::empty(shape, options);
+  const c10::cuda::CUDAStreamGuard guard(c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(c.stream), (c10::DeviceIndex)c.device));
+  at::Tensor t = at::empty(shape, options);
+  if (t.numel() > 0) c10::cuda::CUDACachingAllocator::recordStream(t.storage().data_ptr(), current);
+  return t;
 }
 bool whole_numbers(PyObject* const* a, int n, int* x) {
   for (int i = 0; i < n; ++i) {
@@ -163,7 +178,7 @@ PyObject* append_rope(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     } else {
       if (!strided_rows(a[10], B, n, Hq, c.device, &q)) return nullptr;
       if (a[15] == Py_None) {
-        at::Tensor t = at::empty({B, n, Hq, 128}, THPVariable_Unpack(a[10]).options());
+        at::Tensor t = result_of(c, {B, n, Hq, 128});
         out = t.data_ptr();
         result = THPVariable_Wrap(std::move(t));
         if (!result) return nullptr;
@@ -212,7 +227,7 @@ PyObject* decode_attn_q4(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     if (a[12] != Py_None && !shaped(a[12], at::kFloat, {B, T, Hq}, c.device, &lse)) return nullptr;
     PyObject* result = a[11];
     if (a[11] == Py_None) {
-      at::Tensor t = at::empty({B, T, Hq, 128}, qt->options());
+      at::Tensor t = result_of(c, {B, T, Hq, 128});
       out = t.data_ptr();
       result = THPVariable_Wrap(std::move(t));
       if (!result) return nullptr;
@@ -272,7 +287,7 @@ PyObject* unpack_chunks(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
       if (out[i] != Py_None) {
         if (!shaped(out[i], at::kBFloat16, {S, rows, 128}, c.device, &p[i])) return nullptr;
       } else {
-        made[i] = at::empty({S, rows, 128}, at::TensorOptions().dtype(at::kBFloat16).device(at::kCUDA, (c10::DeviceIndex)c.device));
+        made[i] = result_of(c, {S, rows, 128});
         p[i] = made[i].data_ptr();
       }
     }

@@ -1,4 +1,4 @@
-"""The cache in 4 bits beside pages that were handed back, counts that only the device knows and rows that are not seen."""
+"""The cache in 4 bits beside pages that were handed back, counts that only the device knows, rows that are not seen and other streams."""
 import numpy as np
 import pytest
 import torch
@@ -188,3 +188,68 @@ def test_causal_blocks_with_rows_that_are_not_finite(T, G, n):
     assert np.isnan(got[0, T - 1, G:]).all()
     if T // 2 > 1:
         assert np.isneginf(got[0, T - T // 2:T - 1, G:]).all()
+
+
+# ---- results on another stream ---------------------------------------------------------------------------------------------------------
+
+def freed_block(shape):
+    """the address of a block that the current stream has just given back"""
+    t = torch.empty(shape, dtype=torch.bfloat16, device="cuda")
+    return t.data_ptr()
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_results_of_a_call_on_another_stream_are_that_streams(native, monkeypatch):
+    """a block that the current stream has given back may still be in use there: a call on another stream does not take it for its result"""
+    from paper_2509_21354_b200 import binding as b
+    case = Case(B=2, Hkv=2, n=700, W=60, max_tokens=800)
+    if not native:
+        monkeypatch.setattr(b, "_bind", None)
+    st, side, rope = case.st, torch.cuda.Stream(), b.Rope()
+    q = normal((2, 1, 4, 128), 1)[:, :, :2].contiguous()
+    k, v = normal((2, 1, 2, 128), 2), normal((2, 1, 2, 128), 3)
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    ways = [((2, 1, 2, 128), lambda: [st.decode_attn_q4(0, q, dense=True, stream=side)]),
+            ((2, 1, 2, 128), lambda: [st.append_rope(0, q, k, v, rope, stream=side)[0]]),
+            ((2, 1, 2, 128), lambda: [st.append_rope_next(0, q, k, v, rope, stream=side)]),
+            ((4, 64, 128), lambda: list(st.unpack_chunks(0, 1, 2, stream=side)))]
+    for shape, call in ways:
+        was = freed_block(shape)
+        again = torch.empty(shape, dtype=torch.bfloat16, device="cuda")
+        assert again.data_ptr() == was                      # (the allocator hands the block out again at once)
+        del again
+        results = call()
+        assert all(r.data_ptr() != was for r in results)
+        torch.cuda.synchronize()
+        plain = torch.empty(shape, dtype=torch.bfloat16, device="cuda")
+        assert plain.data_ptr() == was                      # it was there to be taken
+        del plain, results
+    assert st.poll_status() == 0
+
+
+def test_results_of_the_other_calls_on_another_stream():
+    from paper_2509_21354_b200 import binding as b
+    st, side = b.Store(B=2, H=2, C_=64, W=60, max_tokens=800, d_g=64, max_query_tokens=4), torch.cuda.Stream()
+    st.append(0, normal((4, 700, 128), 1), normal((4, 700, 128), 2))
+    one = lambda i: normal((4, 128), i)
+    rows = [one(i) for i in range(3)]
+    block = normal((2, 3, 2, 128), 6)
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    ways = [((4, 128), lambda: st.decode_attn(0, rows[0], stream=side)), ((4, 128), lambda: st.decode_attn_dense(0, rows[0], stream=side)),
+            ((4, 128), lambda: st.decode_step(0, *rows, stream=side)), ((2, 3, 2, 128), lambda: st.decode_attn_block(0, block, dense=True, stream=side))]
+    for shape, call in ways:
+        was = freed_block(shape)
+        result = call()
+        assert result.shape == shape and result.data_ptr() != was
+        torch.cuda.synchronize()
+        assert freed_block(shape) == was
+        del result
+    # the count is a zero that the call's own stream wrote, not one that may come behind its result
+    busy = torch.zeros(1 << 28, device="cuda")
+    for _ in range(20):
+        busy.add_(1.0)
+    _, count = st.reclaim_pages(0, 0, 0, stream=side)
+    side.synchronize()
+    assert int(count) == 0 and st.poll_status() == 0
