@@ -97,7 +97,11 @@ __global__ void __launch_bounds__(PK_WARPS * 32) kve_pack_kernel(LayerView v, Q4
   pdl_launch_dependents();
   pdl_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  if (threadIdx.x == 0) had_packed = *reinterpret_cast<const volatile int32_t*>(v.n_packed);
+  int rows = 0, arrived = 0;
+  if (threadIdx.x == 0) {
+    rows = v.seq_len[0];
+    had_packed = *reinterpret_cast<const volatile int32_t*>(v.n_packed);
+  }
   const int item = blockIdx.x * PK_WARPS + warp;
   const bool live = item < n_units;
   const int per_chunk = v.C / Q4_UNIT_ROWS;
@@ -116,19 +120,22 @@ __global__ void __launch_bounds__(PK_WARPS * 32) kve_pack_kernel(LayerView v, Q4
   }
   // The count of packed chunks goes up when every CTA has read it: a chunk that was not packed before and whose rows are gone has no copy that could stay.
   __syncthreads();
-  if (threadIdx.x == 0) {
-    const int arrived = atomicAdd(ticket, 1);      // (no fence: the barrier has waited for the read, which is all that the last one's write must not pass)
-    if (arrived == (int)gridDim.x - 1) {      // (a replay may find another length, or fewer chunks packed: none is named that has no rows, no gap left)
-      const int now = min(t0 + n_chunks, v.seq_len[0] / v.C);
-      if (had_packed >= t0 && now > had_packed) *v.n_packed = now;
-      *ticket = 0;      // clean for the next launch
-    }
+  if (threadIdx.x == 0) arrived = atomicAdd(ticket, 1);      // (no fence: the barrier has waited for the read, which is all that the last one's write must not pass)
+  auto count = [&]() {      // (the ticket has come back by the time the rows have)
+    if (threadIdx.x != 0 || arrived != (int)gridDim.x - 1) return;
+    const int now = min(t0 + n_chunks, rows / v.C);      // (a replay may find another length, or fewer chunks packed: none is named that has no rows, no gap left)
+    if (had_packed >= t0 && now > had_packed) *v.n_packed = now;
+    *ticket = 0;      // clean for the next launch
+  };
+  if (!live) {
+    count();
+    return;
   }
-  if (!live) return;
   if (!whole) {      // (warp by warp)
     if (!source && target && t >= had_packed)      // 16 rows of two groups that stand for NaN, not for what the page held before
       *reinterpret_cast<uint32_t*>(dst + Q4_CODE_BYTES + lane * 4) = 0x7fff7fffu;
     if (lane == 0 && !(page == -1 && target && discarded(v, s, t))) set_status(v.status, ERR_CAPACITY);
+    count();
     return;
   }
   // (largest, -smallest) of this lane's part of row 2 i + half; then of the whole group, lane by lane: lane 8 g + i has group g of the rows 2 i and 2 i + 1
@@ -180,6 +187,7 @@ __global__ void __launch_bounds__(PK_WARPS * 32) kve_pack_kernel(LayerView v, Q4
       *reinterpret_cast<uint4*>(dst + h * 512 + lane * 16) = make_uint4(w[0], w[1], w[2], w[3]);
     }
   }
+  count();
 }
 
 __global__ void __launch_bounds__(PK_WARPS * 32) kve_unpack_kernel(LayerView v, Q4Pages p, int t0, int n_chunks, int n_units, FastDiv by_units, FastDiv by_chunks,
