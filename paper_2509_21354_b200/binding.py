@@ -641,6 +641,10 @@ def kvE_append_rope_next(st: Store, layer, q, k_new, v_new, rope, positions=None
 
 def kvE_unpack_chunks(st: Store, layer, chunk_begin, chunk_end, k_out=None, v_out=None, stream=None):
     """What the packed chunks stand for: bf16 [S, (chunk_end - chunk_begin) C, 128], keys and values."""
+    if not 0 <= chunk_begin < chunk_end <= st.max_chunks:      # no rows, or refused: no buffers are made for it (an address that is not used)
+        rc = st.lib.kvE_unpack_chunks(st.handle, layer, *(max(-1, min(int(t), 0x7FFFFFFF)) for t in (chunk_begin, chunk_end)), 256, 256, _stream(st, stream))
+        if rc:
+            _check("kvE_unpack_chunks", rc, st.handle)
     if _bind is not None:
         rc, k_out, v_out = _bind.unpack_chunks(*_native(st, "kvE_unpack_chunks", stream), layer, chunk_begin, chunk_end, st.S, st.C, k_out, v_out)
         if rc:

@@ -1,4 +1,4 @@
-"""The cache in 4 bits beside pages that were handed back, counts that only the device knows, rows that are not seen and other streams."""
+"""The cache in 4 bits beside pages that were handed back, counts that only the device knows, rows that are not seen, other streams and ranges that are refused."""
 import numpy as np
 import pytest
 import torch
@@ -253,3 +253,24 @@ def test_results_of_the_other_calls_on_another_stream():
     _, count = st.reclaim_pages(0, 0, 0, stream=side)
     side.synchronize()
     assert int(count) == 0 and st.poll_status() == 0
+
+
+# ---- ranges that are refused -----------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("native", [True, False])
+def test_ranges_of_chunks_to_unpack(native, monkeypatch):
+    from paper_2509_21354_b200 import binding as b
+    case = Case(n=700, W=60)
+    if not native:
+        monkeypatch.setattr(b, "_bind", None)
+    st = case.st
+    for lo, hi, rc in ((2, 1, -1), (-1, 2, -1), (-2, -1, -1), (0, 11, -4), (11, 11, -4), (0, 1 << 20, -4), (0, 1 << 40, -4), (10, 1 << 31, -4)):
+        with pytest.raises(b.KveError) as e:
+            st.unpack_chunks(0, lo, hi)
+        assert e.value.rc == rc
+    for at in (0, 4, 10):
+        k, v = st.unpack_chunks(0, at, at)
+        assert k.shape == v.shape == (2, 0, 128)
+    with pytest.raises(b.KveError):
+        b.Store(B=1, H=1, C_=64, W=0, max_tokens=128, d_g=64).unpack_chunks(0, 0, 0)
+    assert st.unpack_chunks(0, 0, 10)[0].shape == (2, 640, 128) and st.poll_status() == 0
