@@ -290,7 +290,7 @@ typedef struct {
   int32_t n_axes;        /* 1 .. KVE_ROPE_MAX_AXES */
   int32_t layout;        /* KVE_ROPE_* */
   uint8_t axis[64];      /* the axis that pair j follows, < n_axes */
-  double inv_freq[64];   /* radians per position; 0: the pair is not turned */
+  double inv_freq[64];   /* radians per position, finite; 0: the pair is not turned */
 } kvE_rope;
 
 /* bf16 rows of d numbers as a projection leaves them: row (b, token, head) at data + b stride_b + token stride_t + head stride_h

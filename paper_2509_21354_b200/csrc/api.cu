@@ -1,6 +1,7 @@
 // Host side of libkve: the C ABI of include/kve.h.  Validates arguments, tracks per-layer progress
 // (tokens stored, chunks summarised / gated / compacted) and enqueues the kernels.  Allocates no
 // device memory.
+#include <cmath>
 #include <mutex>
 #include <new>
 #include <string>
@@ -916,7 +917,7 @@ int append_rope(kvE_store* st, int layer, const kvE_rows* q, const kvE_rows* k_n
   call.k = rows(*k_new);
   call.v = rows(*v_new);
   for (int j = 0; j < 64; ++j) {
-    if (rope->axis[j] >= rope->n_axes) return KVE_ERR_ARG;
+    if (rope->axis[j] >= rope->n_axes || !std::isfinite(rope->inv_freq[j])) return KVE_ERR_ARG;
     call.axis[j] = rope->axis[j];
     call.turns[j] = rope->inv_freq[j] * 0.15915494309189533576888376337251;      // 1 / (2 pi)
   }
