@@ -337,7 +337,8 @@ typedef struct {
 size_t kvE_q4_workspace_bytes(const kvE_config* cfg, int max_query_tokens);
 
 /* Gives a handle its 4-bit pages (caller-owned DEVICE buffers, borrowed until kvE_destroy); no chunk is packed afterwards, also
- * where the handle had others before.  Synchronises the device.  KVE_ERR_GEOMETRY if C is not a multiple of 16. */
+ * where the handle had others before; launches captured with those must not be replayed.  Synchronises the device.  KVE_ERR_GEOMETRY if C is not a
+ * multiple of 16. */
 int kvE_attach_q4(kvE_store* st, const kvE_q4_buffers* buf);
 
 /* Chunks [chunk_begin, chunk_end) of every sequence of `layer` to 4 bits, from their bf16 pages, which stay as they are
@@ -364,8 +365,9 @@ int kvE_packed_chunks(const kvE_store* st, int layer, int* n_packed);
  *   causal != 0: the block's tokens are the newest of the cache and see it up to themselves; KVE_ERR_STATE if fewer rows than
  *   n_query_tokens lie behind the packed and listed chunks (a replay that comes to that sets KVE_ERR_CAPACITY).  Keys and values of a token are nothing to the
  *   tokens in front of it, infinities and NaN included.
- *   Sums in fp32, weights of packed rows to 11 bits (of bf16 rows to 16), one bf16 rounding of the result: values between 2^-60 and 2^60 in
- *   magnitude, or 0.  (Scales below that lose bits; sums of larger bf16 rows beside them may overflow.)  A row that sees nothing gives 0 and lse = -inf.
+ *   Sums in fp32, one bf16 rounding of the result.  A bf16 row's weight has 16 bits.  A packed row's weight times scale has 11, or is off by 2^-21 of the
+ *   largest such product that the query row meets in the group, whatever the sizes of other rows and groups; products below 2^-80 of the largest weight count
+ *   as 0.  Values between 2^-60 and 2^60 in magnitude, or 0 (sums of larger bf16 rows may overflow).  A row that sees nothing gives 0 and lse = -inf.
  *   q, out: DEVICE bf16 [B][n_query_tokens][Hq][d], on 16 bytes; lse: DEVICE fp32 [B][n_query_tokens][Hq] or NULL.
  *   KVE_ERR_STATE without kvE_attach_q4, KVE_ERR_CAPACITY if n_query_tokens exceeds max_query_tokens. */
 int kvE_decode_attn_q4(kvE_store* st, int layer, const void* q, int n_query_tokens, int dense, int causal, void* out, float* lse,

@@ -1002,8 +1002,11 @@ bool too_many_units(const kvE_store* st, int chunks) { return 2LL * st->S * chun
 // How an attention launch is cut up: every sequence into k equal parts, `runs` CTAs (for every group of query rows) with a contiguous run of them each.
 // The cheaper of two ways, in microseconds: a number of CTAs of its own for every sequence, or one resident wave that goes from sequence to sequence, which costs
 // a CTA 3 us a turn (state to shared memory, another's query rows, a first tile that raises every reference) and 2.5 us where records meet.
-// Measured (graph of launches): 8 sequences of 100003 rows, 4 query rows: 16 CTAs each 30.8 us, 8 each 52.8; 64 of 4099: 2 each 18.4, wave 24.3; 128 of 4167, half kept:
-// 1 each 17.4, wave of halves 23.0; 512 of 16512, half kept: wave of halves 156, of fifths 162, of whole sequences 173, 1 each after another 181.
+// Measured (graph of launches; the rule's choice first): 8 sequences of 2048 rows: 15 CTAs each 9.3 us, 12 9.2, 10 and 18 9.5; 8 of 100003, 4 query rows: 18 each 30.5, 16 32.0,
+// 12 38.5; 64 of 4099: 2 each 18.2, 1 23.9, wave of quarters 21.5; 128 of 4167, half kept: 1 each 17.4, wave of halves 22.6; 256 of 8320: wave of fifteenths 64.9, of quarters 64.5,
+// of halves 71.8; 512 of 16512, half kept: wave of thirteenths 155.5, of halves 153.5, of fifths 159.8, of whole sequences 171.4; 128 of 16512, 28 query rows: wave of fifteenths
+// 231, of fifths 238, of halves 264; 128 of 8320, 8 and 16 rows: 1 each 41.3 and 65.5, waves 46.4 and 72.6 at best.  The model's times are up to 35 us off (it knows neither how the
+// copies share the memory nor how many sequences meet others); what it is asked is their order, and no other cut that was tried is faster than its choice by more than 1.5 %.
 struct Q4Cut { int k, runs; };
 Q4Cut q4_cut(const kvE_store* st, const LayerState& ls, bool dense, int rows) {
   const int C = st->cfg.C;

@@ -11,12 +11,14 @@
 //  * all products are m16n8k16 MMAs.  Three forms, by the query rows of a CTA (q4_attn_shape), because the tensor core takes 16 rows by 8 columns whether they are used or not:
 //      1 to 4 rows: the cache on the M side (keys: 16 rows; values, transposed: 16 dims), the queries in the eight columns: the four rows twice, once for either group of 64
 //        dims (q is zero in the other half; the weights have the group's scale), so that a lane has to do with one group only: half of the scales, weights and conversions.
-//        16 sequences x 32 heads x 16512 rows, half of the chunks kept: 160 us; with the rows once in eight columns 170.
-//      5 to 8 rows: the same, a row a column.  128 sequences x 8320 rows: 43 us; with the queries on the M side 65.
+//        16 sequences x 32 heads x 16512 rows, half of the chunks kept: 156 us (when both were built: 160, with the rows once in eight columns 170).
+//      5 to 8 rows: the same, a row a column.  128 sequences x 8320 rows: 41 us (when both were built: 43, with the queries on the M side 65).
 //        In both the logits' accumulator becomes the weights' operand through movmatrix, in registers.
 //      9 to 16 rows: the queries on the M side, where the logits' accumulator is the weights' operand as it stands.  The lowest numbers' share of a logit, minus the
-//        reference, is a product too, of three bf16 planes.  128 sequences x 8320 rows, 16 rows: 66 us; as two blocks of columns of the form above 72.
-//  * the weights p s F of packed rows are fp16: 11 bits, whose rounding (2^-12 a row) stays far below the result's own (2^-9).  F, a power of two per
+//        reference, is a product too, of three bf16 planes.  128 sequences x 8320 rows, 16 rows: 66 us (as two blocks of columns of the form above 72).
+//  * the weights p s F of packed rows are fp16: 11 bits, off by half a step (2^-11 of the weight) at most, for half the MMAs of two planes.  What a weight multiplies is
+//    c s, up to 15 steps above the lowest number, so for values around 0 its rounding counts a few times: normal values make 5e-4 (relative, rms) of it before the result is
+//    rounded to bf16 (1.6e-3), 1.7e-3 with both.  F, a power of two per
 //    warp, query row and group, keeps them between what fp16 overflows at and where it runs out of bits (qa_factor).  bf16 rows take their weights as two bf16 planes.
 //  * a tile's products with the values are summed from zero and added to the accumulator by ordinary additions: the tensor core cuts off what lies below
 //    the last bit of its accumulator at every step, always in one direction.

@@ -36,7 +36,7 @@ __global__ void __launch_bounds__(RP_THREADS, RP_CTAS) kve_append_rope_kernel(La
   const int tid = threadIdx.x, x = tid & 7;
   const int tok0 = blockIdx.x * a.tokens_per_cta, n_tok = min(a.tokens_per_cta, a.n_tokens - tok0);
   const int rows = a.Hq + 2 * v.H, n_items = n_tok * rows;
-  const int off_a = 8 * x, off_b = 64 + 8 * x;      // the thread's two pieces of a row (adjacent pairs too: side by side they made half of every 32-byte sector a load of its own, 257 -> 265 us)
+  const int off_a = 8 * x, off_b = 64 + 8 * x;      // the thread's two pieces of a row (adjacent pairs too: side by side they made half of every 32-byte sector a load of its own, 254 -> 264 us)
 
   // a row under way: its numbers, its token, where it goes (null: nowhere), whether it turns
   struct Row { uint4 lo, hi; uint16_t* dst; int tok; bool turns; };
@@ -169,8 +169,8 @@ cudaError_t launch_append_rope(const LayerView& v, const RopeCall& call, bool ne
   static_cast<RopeCall&>(a) = call;
   a.n_tokens = v.B * a.n_new;
   // one pass of the CTA, or one token; with tokens for two full waves, six passes (the rows of one pass are fetched while the ones before are turned and stored, and the
-  // angles of a few tokens take as long as those of one).  16 x 4096 tokens of 12 rows: 72 us, with one and a half passes 80; of 6 rows 48 and 65; of 9 rows 62 and 72;
-  // 8 x 4096 of 96 rows 254, with three passes 396, with twelve 261
+  // angles of a few tokens take as long as those of one).  8 x 4096 tokens of 96 rows: 254 us, with three passes 260, with twelve 262; 16 x 4096 of 9 rows 58, with three 60; of 6 and
+  // 12 rows 45 and 70, with three passes as with six.  At the device's length 293, 54 (6 rows), 67, 81: a CTA waits for its stores before it takes its ticket
   int per = RP_ROWS / rows, most = a.n_tokens / (2 * RP_CTAS * sm_count());
   const int want = (6 * RP_ROWS + rows - 1) / rows;
   if (most > want) most = want;
