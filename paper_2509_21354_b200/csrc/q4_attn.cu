@@ -18,8 +18,8 @@
 //        reference, is a product too, of three bf16 planes.  128 sequences x 8320 rows, 16 rows: 66 us (as two blocks of columns of the form above 72).
 //  * the weights p s F of packed rows are fp16: 11 bits, off by half a step (2^-11 of the weight) at most, for half the MMAs of two planes.  What a weight multiplies is
 //    c s, up to 15 steps above the lowest number, so for values around 0 its rounding counts a few times: normal values make 5e-4 (relative, rms) of it before the result is
-//    rounded to bf16 (1.6e-3), 1.7e-3 with both.  F, a power of two per
-//    warp, query row and group, keeps them between what fp16 overflows at and where it runs out of bits (qa_factor).  bf16 rows take their weights as two bf16 planes.
+//    rounded to bf16 (1.6e-3), 1.7e-3 with both.  F, a power of two per warp, query row and group, keeps them between what fp16 overflows at and where it runs out of
+//    bits (qa_factor).  bf16 rows take their weights as two bf16 planes.
 //  * a tile's products with the values are summed from zero and added to the accumulator by ordinary additions: the tensor core cuts off what lies below
 //    the last bit of its accumulator at every step, always in one direction.
 //  * the reference of the softmax is raised only when a logit passes it by more than 2^8 (a vote), not at every tile.
